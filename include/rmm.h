@@ -238,6 +238,82 @@ size_t rmm_product_host_workspace_bytes(int64_t M, int64_t K, int64_t N);
 int rmm_product_host(const void *A_host, const void *B_host, int64_t M, int64_t K, int64_t N, double rho, int copy_B,
                      void *Y_host, int32_t *idx_host, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- from a projection's heads to attention over a paged cache held in 4 bits --------------------------------------------------
+ *
+ * Rows of heads: element (b, h, i, d) at ptr + (b*stride[0] + h*stride[1] + i*stride[2] + d) elements, bf16 or fp32.  Strides are
+ * non-negative; rows on 16-byte boundaries are read and written in whole vectors, others element by element. */
+typedef struct {
+    void *ptr;
+    int32_t dtype;      /* RMM_BF16 or RMM_F32 */
+    int64_t B, H, L, D; /* sequences, heads, rows (tokens) of a sequence, columns of a head */
+    int64_t stride[3];  /* batch, head, row */
+} rmm_heads_t;
+
+/* What turns with the position.  Row p of `table` (fp32) holds the rot/2 cosines of position p's angles, then the rot/2 sines (any
+ * scaling of the angles or of their size is in the table).  A head's first `rot` columns turn in pairs (d, d + rot/2), or
+ * (2d, 2d + 1) if interleaved; the rest stay.  rot is a multiple of 16.  table NULL: no rotation. */
+typedef struct {
+    const float *table;
+    int64_t table_rows, table_stride, rot;
+    int32_t interleaved;
+    int32_t weight_dtype;      /* of the norm's weights: RMM_BF16 or RMM_F32 */
+    double eps;
+    const int32_t *positions;  /* rmm_qk_norm_rope only: position of row (b, i) at [b*pos_stride[0] + i*pos_stride[1]]; NULL: i */
+    int64_t pos_stride[2];
+} rmm_rope_t;
+
+/* Q' = rotation(norm(Q)), K' = rotation(norm(K)) for every head's row in one pass:  y = x w / sqrt(mean x^2 + eps) with one weight
+ * [D] for all query heads and one for all key heads (contiguous; NULL: that side is not normalised), then
+ * (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin) for each pair.  Taken in fp32, rounded once.  D is a multiple of 8, at most
+ * 256.  Q_out and K_out have the shapes of Q and K, bf16 or fp32 (both the same), and may be the inputs themselves.  K, K_out NULL:
+ * queries only.  A row whose position is outside the table is not written and reported as RMM_ERR_BOUNDS.
+ * The workspace is only used for the status word: RMM_WS_HEADER_BYTES. */
+int rmm_qk_norm_rope(const rmm_heads_t *Q, const rmm_heads_t *K, const void *q_weight, const void *k_weight, const rmm_rope_t *rope,
+                     const rmm_heads_t *Q_out, const rmm_heads_t *K_out, void *ws, size_t ws_bytes, void *stream);
+
+/* A paged cache.  Every 64 columns of a (token, head) share a step s and a least value m, both bf16, and hold a code n of 4 bits a
+ * column:  x = m + s n,  m = min x,  s = bf16((max x - m) / 15),  n = min(15, round((x - m) / s)), halves to the even code, 0 where
+ * s = 0 (4.5 bits a value; off by at most 0.53 s).  Pages hold `page` tokens of every head: per head page/16 blocks of 18 Dh
+ * contiguous bytes, 16 tokens each (keys' codes, values' codes, keys' steps, values' steps; csrc/kv4.cuh has their order).
+ * Token t of sequence b lies in page pages[b*pages_stride + t/page], row t % page.  Dh is 64, 128 or 256; page a power of two >= 16.
+ * The sequences' sizes live on the device, so that a captured graph follows them:
+ *   lengths[b]  tokens of sequence b, those that the call appends, asks from or reads included
+ *   new_len[b]  how many of them are the call's rows: row i < new_len[b] is token lengths[b] - new_len[b] + i.  NULL: all L rows.
+ * Entries of `pages` behind a sequence's last token are not read.  A length outside [0, max_pages*page], a row count outside [0, L],
+ * and a page outside the pool are reported as RMM_ERR_BOUNDS; the call then keeps within the bounds (tokens of such a page are
+ * skipped).  Pages may be shared by sequences that read them; rmm_kv4_append must not write one token twice. */
+typedef struct {
+    void *pool;                        /* 16-byte aligned */
+    int64_t n_pages, page, Hkv, Dh;
+    int64_t page_stride, head_stride;  /* bytes, multiples of 16 */
+    const int32_t *pages;
+    int64_t B, max_pages, pages_stride;
+    const int32_t *lengths, *new_len;
+} rmm_kv4_t;
+
+/* Keys and values into the cache: K [B,Hkv,L,Dh] is normalised (k_weight) and rotated as rmm_qk_norm_rope does, at its token's
+ * place in the sequence (rope->positions is not used; NULL rope: neither), rounded to bf16 as the 64-bit result would be, and
+ * quantised; V [B,Hkv,L,Dh] is rounded to bf16 and quantised.  K and V share a dtype.  K_held, V_held (bf16, or both NULL) receive
+ * what the cache then holds, rounded to bf16, for the prompt's own attention; rows behind new_len[b] are zeros there.  A row whose
+ * place is negative or outside the table is skipped and reported as RMM_ERR_BOUNDS.  Workspace: RMM_WS_HEADER_BYTES. */
+int rmm_kv4_append(const rmm_heads_t *K, const rmm_heads_t *V, const rmm_kv4_t *cache, const void *k_weight, const rmm_rope_t *rope,
+                   const rmm_heads_t *K_held, const rmm_heads_t *V_held, void *ws, size_t ws_bytes, void *stream);
+
+/* Keys and values of the call's rows back from the cache: K, V [B,Hkv,L,Dh], bf16 or fp32, m + s n in fp32 rounded once; rows behind
+ * new_len[b], and tokens of a page outside the pool, are zeros.  Workspace: RMM_WS_HEADER_BYTES. */
+int rmm_kv4_read(const rmm_kv4_t *cache, const rmm_heads_t *K, const rmm_heads_t *V, void *ws, size_t ws_bytes, void *stream);
+
+/* Reduced attention of Sec. 3.3 (rho_t = 1) of bf16 rows Q [B,Hq,L,Dh] over the cache, O [B,Hq,L,Dh] bf16: as rmm_reduced_attn over
+ * the values that the cache holds, with Lk = lengths[b]; causal: row i < new_len[b] sees the tokens up to its own.  A row that sees
+ * no token, and the rows behind new_len[b], are zeros.  rho_d < 1 keeps ceil(rho_d Dh) features of each query head, chosen from
+ * its new_len[b] rows, of which there may be 16 at most (L <= 16); idx_feat int32 [B,Hq,kd] (or NULL) receives them (not for
+ * sequences without rows).  Any L is taken, 8 or 16 query rows of a kv head at a time, so that a long chunk reads the cache many times over:
+ * from some 64 rows on rmm_kv4_read and rmm_reduced_attn are faster.  Softmax weights times a value's step are rounded to fp16; logits,
+ * sums and O are fp32.  Inputs are finite, cached steps between 2^-80 and 2^60. */
+size_t rmm_kv4_attn_workspace_bytes(const rmm_heads_t *Q, const rmm_kv4_t *cache);
+int rmm_kv4_attn(const rmm_heads_t *Q, const rmm_kv4_t *cache, int causal, double rho_d, const rmm_heads_t *O, int32_t *idx_feat,
+                 void *ws, size_t ws_bytes, void *stream);
+
 /* Copy the device status word of a workspace to *device_status (an rmm_status_t) and clear it.  If the word was set,
  * the whole header (the arrival counters too: a kernel that gave up may have left them half way) is zeroed, which
  * makes the workspace usable again.  Synchronous: call it after the stream the workspace was used on has been
@@ -249,7 +325,8 @@ int rmm_status_read(void *ws, int *device_status);
  * first used.  rmm_debug_control("wait_limit_ms", x) overrides the bound for later launches (0 = back to the default);
  * rmm_debug_control("withhold", w) makes block 0 of one kernel family never request its first tile (w = 1 tensor-core
  * product, 2 score pass, 3 fused attention, 4 one-launch front end of rmm_product, 5 streaming column gather, 6 streaming
- * 8-bit gather; 0 = off, -1 = back to the environment variable RMM_TEST_WITHHOLD = gemm | score | attn | front | pack | quant),
+ * 8-bit gather, 7 attention over a 4-bit cache; 0 = off, -1 = back to the environment variable
+ * RMM_TEST_WITHHOLD = gemm | score | attn | front | pack | quant | kv4),
  * so that the waits behind
  * that tile run out: the kernel must then report RMM_ERR_TIMEOUT in the status word, release what it holds and return.
  * Results of such a call are undefined; rmm_status_read clears the workspace header, after which the workspace is

@@ -10,12 +10,18 @@ from .binding import (  # noqa: F401
     rmm,
     rmm_debug_control,
     rmm_keep_count,
+    rmm_kv4_append,
+    rmm_kv4_attn,
+    rmm_kv4_pool,
+    rmm_kv4_read,
     rmm_launch_count,
     rmm_product,
     rmm_product_host,
+    rmm_qk_norm_rope,
     rmm_reduced_attn,
     rmm_reduced_gemm,
     rmm_reduced_gemm_q8,
+    rmm_rope_table,
     rmm_score,
     rmm_score_select,
     rmm_score_select_static,

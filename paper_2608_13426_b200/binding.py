@@ -50,12 +50,31 @@ class rmm_attn_desc_t(ctypes.Structure):
                 ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64 * 3)]
 
 
+class rmm_heads_t(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("B", ctypes.c_int64), ("H", ctypes.c_int64),
+                ("L", ctypes.c_int64), ("D", ctypes.c_int64), ("stride", ctypes.c_int64 * 3)]
+
+
+class rmm_rope_t(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_rows", ctypes.c_int64), ("table_stride", ctypes.c_int64),
+                ("rot", ctypes.c_int64), ("interleaved", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("eps", ctypes.c_double), ("positions", ctypes.c_void_p), ("pos_stride", ctypes.c_int64 * 2)]
+
+
+class rmm_kv4_t(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page", ctypes.c_int64), ("Hkv", ctypes.c_int64),
+                ("Dh", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("pages", ctypes.c_void_p), ("B", ctypes.c_int64), ("max_pages", ctypes.c_int64),
+                ("pages_stride", ctypes.c_int64), ("lengths", ctypes.c_void_p), ("new_len", ctypes.c_void_p)]
+
+
 EXPORTS = ["rmm_keep_count", "rmm_score_workspace_bytes", "rmm_score", "rmm_select_workspace_bytes", "rmm_select",
            "rmm_score_select_workspace_bytes", "rmm_score_select", "rmm_score_select_static",
            "rmm_score_select_static_capacity", "rmm_score_select_static_status", "rmm_reduced_gemm_workspace_bytes",
            "rmm_reduced_gemm", "rmm_reduced_gemm_scored_workspace_bytes", "rmm_reduced_gemm_scored",
            "rmm_reduced_gemm_q8_workspace_bytes", "rmm_reduced_gemm_q8", "rmm_reduced_attn_workspace_bytes", "rmm_reduced_attn",
-           "rmm_product_workspace_bytes", "rmm_product", "rmm_product_host_workspace_bytes", "rmm_product_host", "rmm_status_read", "rmm_last_error",
+           "rmm_product_workspace_bytes", "rmm_product", "rmm_product_host_workspace_bytes", "rmm_product_host", "rmm_qk_norm_rope",
+           "rmm_kv4_append", "rmm_kv4_read", "rmm_kv4_attn_workspace_bytes", "rmm_kv4_attn", "rmm_status_read", "rmm_last_error",
            "rmm_launch_count", "rmm_debug_control", "rmm_profile_kernels", "rmm_profile_count", "rmm_profile_name"]
 
 _lib = None
@@ -103,6 +122,13 @@ def lib() -> ctypes.CDLL:
     L.rmm_product_host_workspace_bytes.argtypes = [i64, i64, i64]
     L.rmm_product_host_workspace_bytes.restype = sz
     L.rmm_product_host.argtypes = [vp, vp, i64, i64, i64, dbl, i32, vp, vp, vp, sz, vp]
+    hp, rp, cp = ctypes.POINTER(rmm_heads_t), ctypes.POINTER(rmm_rope_t), ctypes.POINTER(rmm_kv4_t)
+    L.rmm_qk_norm_rope.argtypes = [hp, hp, vp, vp, rp, hp, hp, vp, sz, vp]
+    L.rmm_kv4_append.argtypes = [hp, hp, cp, vp, rp, hp, hp, vp, sz, vp]
+    L.rmm_kv4_read.argtypes = [cp, hp, hp, vp, sz, vp]
+    L.rmm_kv4_attn_workspace_bytes.argtypes = [hp, cp]
+    L.rmm_kv4_attn_workspace_bytes.restype = sz
+    L.rmm_kv4_attn.argtypes = [hp, cp, i32, dbl, hp, vp, vp, sz, vp]
     L.rmm_status_read.argtypes = [vp, ctypes.POINTER(i32)]
     L.rmm_last_error.restype = ctypes.c_char_p
     L.rmm_launch_count.restype = i64
@@ -479,6 +505,187 @@ def rmm_reduced_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: 
                                   idx_feat.data_ptr() if idx_feat is not None else None,
                                   idx_tok.data_ptr() if idx_tok is not None else None, p, nb, _stream()))
     return (O, idx_feat, idx_tok) if want_idx else O
+
+
+def _on_device(f):
+    """The call runs on its first tensor's device and that device's current stream, whichever device is current."""
+    @functools.wraps(f)
+    def call(first, *args, **kwargs):
+        if isinstance(first, torch.Tensor) and first.is_cuda and first.get_device() != torch._C._cuda_getDevice():
+            with torch.cuda.device(first.get_device()):
+                return f(first, *args, **kwargs)
+        return f(first, *args, **kwargs)
+    return call
+
+
+def _heads(t: torch.Tensor, name: str, device: torch.device) -> rmm_heads_t:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device or t.dim() != 4:
+        raise RmmError(RMM_ERR_INVALID_ARG, f"{name} must be a 4-D tensor [B, H, L, D] on the call's CUDA device")
+    b, h, l, d = t.shape
+    sb, sh, sl, sd = t.stride()
+    if (sd != 1 and d > 1) or t.dtype not in (torch.bfloat16, torch.float32):
+        raise RmmError(RMM_ERR_UNSUPPORTED, f"{name} must be bf16 or fp32 with a contiguous last dim")
+    return rmm_heads_t(t.data_ptr(), _DTYPE_CODES[t.dtype], b, h, l, d, (ctypes.c_int64 * 3)(sb, sh, sl))
+
+
+def _ints(t: torch.Tensor, name: str, shape, device: torch.device) -> int:
+    if (not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.device != device or tuple(t.shape) != shape
+            or (t.stride(-1) != 1 and shape[-1] > 1)):
+        raise RmmError(RMM_ERR_INVALID_ARG, f"{name} must be an int32 tensor {list(shape)} on the call's CUDA device, last dim contiguous")
+    return t.data_ptr()
+
+
+def _weights(ws, D: int, device: torch.device):
+    """(their common dtype code, addresses or None)"""
+    code, ptrs = None, []
+    for w in ws:
+        if w is None:
+            ptrs.append(None)
+            continue
+        if (not isinstance(w, torch.Tensor) or w.shape != (D,) or w.device != device or (D > 1 and w.stride(0) != 1)
+                or w.dtype not in (torch.bfloat16, torch.float32)):
+            raise RmmError(RMM_ERR_INVALID_ARG, f"norm weights must be contiguous bf16 or fp32 tensors of {D} elements on the call's CUDA device")
+        if code not in (None, _DTYPE_CODES[w.dtype]):
+            raise RmmError(RMM_ERR_UNSUPPORTED, "both norm weights must have one dtype")
+        code = _DTYPE_CODES[w.dtype]
+        ptrs.append(w.data_ptr())
+    return RMM_F32 if code is None else code, ptrs
+
+
+def _rope(table, interleaved, weight_dtype, eps, device: torch.device) -> rmm_rope_t:
+    r = rmm_rope_t(None, 0, 0, 0, int(bool(interleaved)), weight_dtype, float(eps), None, (ctypes.c_int64 * 2)(0, 0))
+    if table is not None:
+        if (not isinstance(table, torch.Tensor) or table.dim() != 2 or table.dtype != torch.float32 or table.device != device
+                or table.stride(1) != 1):
+            raise RmmError(RMM_ERR_INVALID_ARG, "the rotation's table must be an fp32 tensor [positions, rot] on the call's CUDA device, rows contiguous")
+        r.table, r.table_rows, r.rot = table.data_ptr(), table.shape[0], table.shape[1]
+        r.table_stride = table.stride(0) if table.shape[0] > 1 else table.shape[1]
+    return r
+
+
+def _kv4(pool, pages, lengths, new_len, device: torch.device) -> rmm_kv4_t:
+    if not isinstance(pool, torch.Tensor) or pool.dim() != 4 or pool.dtype != torch.uint8 or pool.device != device or not pool.is_cuda:
+        raise RmmError(RMM_ERR_INVALID_ARG, "the pool must be a uint8 tensor [pages, Hkv, page / 16, 18 Dh] on the call's CUDA device (rmm_kv4_pool)")
+    n, hkv, blocks, size = pool.shape
+    sp, sh, sb, s1 = pool.stride()
+    if size % 18 or min(n, hkv, blocks, size) < 1 or s1 != 1 or (blocks > 1 and sb != size):
+        raise RmmError(RMM_ERR_INVALID_ARG, "the pool's blocks must have 18 Dh contiguous bytes and follow one another")
+    if not isinstance(pages, torch.Tensor) or pages.dim() != 2:
+        raise RmmError(RMM_ERR_INVALID_ARG, "pages must be an int32 tensor [B, max_pages]")
+    b, most = pages.shape
+    return rmm_kv4_t(pool.data_ptr(), n, 16 * blocks, hkv, size // 18, sp if n > 1 else hkv * blocks * size, sh if hkv > 1 else blocks * size,
+                     _ints(pages, "pages", (b, most), device), b, most, pages.stride(0) if b > 1 else most,
+                     _ints(lengths, "lengths", (b,), device), None if new_len is None else _ints(new_len, "new_len", (b,), device))
+
+
+def rmm_rope_table(positions: int, rot: int, base: float = 10000.0, device=None) -> torch.Tensor:
+    """fp32 [positions, rot] for the rotation: cosines of p base^(-2 j / rot), j < rot / 2, then their sines; taken in 64 bits.  Any
+    other table of that form serves as well (scaled angles, scaled sizes)."""
+    inv = float(base) ** (-torch.arange(0, rot, 2, device=device, dtype=torch.float64) / rot)
+    angles = torch.arange(positions, device=device, dtype=torch.float64)[:, None] * inv
+    return torch.cat([angles.cos(), angles.sin()], 1).float()
+
+
+@_on_device
+def rmm_qk_norm_rope(Q: torch.Tensor, K: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                     k_weight: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                     eps: float = 1e-6, interleaved: bool = False, out_dtype: Optional[torch.dtype] = None, inplace: bool = False,
+                     ws: Optional[torch.Tensor] = None):
+    """RMS norm of every head's rows and the position rotation in one pass.  Q [B,Hq,L,D], K [B,Hkv,L,D] or None, bf16 or fp32, last
+    dim contiguous; weights [D] (None: that side is not normalised); rope fp32 [P, rot] (rmm_rope_table; None: no rotation);
+    positions int32 [B, L] or [L] (None: row i is at position i).  Returns (Q', K'), or Q' without K: new contiguous tensors in
+    out_dtype (the inputs' own if None), or with inplace the inputs themselves."""
+    device = Q.device if isinstance(Q, torch.Tensor) else None
+    q = _heads(Q, "Q", device)
+    k = None if K is None else _heads(K, "K", device)
+    code, (qw, kw) = _weights((q_weight, k_weight), q.D, device)
+    r = _rope(rope, interleaved, code, eps, device)
+    if positions is not None:
+        p = positions.unsqueeze(0) if isinstance(positions, torch.Tensor) and positions.dim() == 1 else positions
+        if (not isinstance(p, torch.Tensor) or p.dtype != torch.int32 or p.device != device or p.dim() != 2 or p.shape[0] not in (1, q.B)
+                or p.shape[1] != q.L):
+            raise RmmError(RMM_ERR_INVALID_ARG, f"positions must be an int32 tensor [{q.B}, {q.L}] or [{q.L}] on the call's CUDA device")
+        r.positions = p.data_ptr()
+        r.pos_stride = (ctypes.c_int64 * 2)(0 if p.shape[0] == 1 else p.stride(0), p.stride(1))
+    if inplace:
+        if out_dtype not in (None, Q.dtype):
+            raise RmmError(RMM_ERR_INVALID_ARG, "in place the dtype stays")
+        Qo, Ko, qo, ko = Q, K, q, k
+    else:
+        dt = Q.dtype if out_dtype is None else out_dtype
+        Qo = _out(tuple(Q.shape), dt, Q)
+        Ko = None if K is None else _out(tuple(K.shape), dt, K)
+        qo, ko = _heads(Qo, "Q", device), None if K is None else _heads(Ko, "K", device)
+    ws = workspace(0, device) if ws is None else ws
+    w, nb = _ws_ptr(ws)
+    _check(lib().rmm_qk_norm_rope(q, k, qw, kw, r, qo, ko, w, nb, _stream()))
+    return Qo if K is None else (Qo, Ko)
+
+
+def rmm_kv4_pool(n_pages: int, Hkv: int, Dh: int, page: int = 64, device=None) -> torch.Tensor:
+    """Memory for n_pages pages of a 4-bit cache: uint8 [n_pages, Hkv, page / 16, 18 Dh] on the current CUDA device or `device`."""
+    if page < 16 or page & (page - 1) or Dh not in (64, 128, 256):
+        raise RmmError(RMM_ERR_UNSUPPORTED, "page must be a power of two from 16 on, Dh 64, 128 or 256")
+    return torch.zeros(n_pages, Hkv, page // 16, 18 * Dh, dtype=torch.uint8, device="cuda" if device is None else device)
+
+
+@_on_device
+def rmm_kv4_append(K: torch.Tensor, V: torch.Tensor, pool: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor,
+                   new_len: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
+                   eps: float = 1e-6, interleaved: bool = False, want_values: bool = False, ws: Optional[torch.Tensor] = None):
+    """K, V [B,Hkv,L,Dh] (bf16 or fp32) into a paged 4-bit cache; keys are normalised (k_weight) and rotated (rope) on the way.
+    pages int32 [B, max_pages] holds page numbers of `pool`; lengths int32 [B] counts each sequence's tokens with the new ones, which
+    are the first new_len[b] rows (None: all L): row i becomes token lengths[b] - new_len[b] + i and is rotated at that position.
+    With want_values returns (K', V') bf16 [B,Hkv,L,Dh]: what the cache holds for these rows (zeros behind new_len)."""
+    device = K.device if isinstance(K, torch.Tensor) else None
+    k, v = _heads(K, "K", device), _heads(V, "V", device)
+    c = _kv4(pool, pages, lengths, new_len, device)
+    code, (kw,) = _weights((k_weight,), k.D, device)
+    r = _rope(rope, interleaved, code, eps, device)
+    Ko = Vo = ko = vo = None
+    if want_values:
+        Ko, Vo = _out(tuple(K.shape), torch.bfloat16, K), _out(tuple(K.shape), torch.bfloat16, K)
+        ko, vo = _heads(Ko, "K", device), _heads(Vo, "V", device)
+    ws = workspace(0, device) if ws is None else ws
+    w, nb = _ws_ptr(ws)
+    _check(lib().rmm_kv4_append(k, v, c, kw, r, ko, vo, w, nb, _stream()))
+    return (Ko, Vo) if want_values else None
+
+
+@_on_device
+def rmm_kv4_read(pool: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor, new_len: Optional[torch.Tensor] = None,
+                 rows: int = 1, out_dtype: torch.dtype = torch.bfloat16, ws: Optional[torch.Tensor] = None):
+    """(K, V) [B, Hkv, rows, Dh] of the last new_len[b] tokens of every sequence (None: of the last `rows`), zeros behind them; with
+    new_len = lengths whole sequences.  What a long chunk's rmm_reduced_attn reads."""
+    device = pool.device if isinstance(pool, torch.Tensor) else None
+    c = _kv4(pool, pages, lengths, new_len, device)
+    K, V = (_out((c.B, c.Hkv, int(rows), c.Dh), out_dtype, pool) for _ in range(2))
+    ws = workspace(0, device) if ws is None else ws
+    w, nb = _ws_ptr(ws)
+    _check(lib().rmm_kv4_read(c, _heads(K, "K", device), _heads(V, "V", device), w, nb, _stream()))
+    return K, V
+
+
+@_on_device
+def rmm_kv4_attn(Q: torch.Tensor, pool: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor, new_len: Optional[torch.Tensor] = None,
+                 causal: bool = True, rho_d: float = 1.0, want_idx: bool = False, ws: Optional[torch.Tensor] = None):
+    """Reduced attention of Q [B,Hq,L,Dh] bf16 over the paged 4-bit cache: rows i < new_len[b] (None: all L) are the last tokens of
+    lengths[b]; causal rows see the tokens up to their own, the others all.  Returns O [B,Hq,L,Dh] bf16 (zeros where a row sees
+    nothing, and behind new_len), or (O, idx_feat) with want_idx.  A call that is captured into a graph needs a `ws` of its own
+    that lives as long as the graph, as do calls that may overlap."""
+    device = Q.device if isinstance(Q, torch.Tensor) else None
+    q = _heads(Q, "Q", device)
+    c = _kv4(pool, pages, lengths, new_len, device)
+    O = _out(tuple(Q.shape), torch.bfloat16, Q)
+    o = _heads(O, "O", device)
+    need = lib().rmm_kv4_attn_workspace_bytes(q, c)
+    if need == 0:
+        _check(lib().rmm_kv4_attn(q, c, 0, 1.0, o, None, None, 0, None) or RMM_ERR_INVALID_ARG)
+    idx = _out((q.B, q.H, rmm_keep_count(rho_d, q.D)), torch.int32, Q) if want_idx else None
+    ws = workspace(need, device) if ws is None else ws
+    w, nb = _ws_ptr(ws)
+    _check(lib().rmm_kv4_attn(q, c, int(bool(causal)), float(rho_d), o, None if idx is None else idx.data_ptr(), w, nb, _stream()))
+    return (O, idx) if want_idx else O
 
 
 def rmm_product_host(A_host: torch.Tensor, B_host: torch.Tensor, rho: float, Y_host: torch.Tensor,

@@ -91,6 +91,7 @@ int debug_withhold()
         if (strcmp(e, "front") == 0) return (int)WITHHOLD_FRONT;
         if (strcmp(e, "pack") == 0) return (int)WITHHOLD_PACK;
         if (strcmp(e, "quant") == 0) return (int)WITHHOLD_QUANT;
+        if (strcmp(e, "kv4") == 0) return (int)WITHHOLD_KV4;
         return 0;
     }();
     return which;
@@ -612,7 +613,7 @@ int rmm_debug_control(const char *key, double value)
     }
     if (strcmp(key, "withhold") == 0) {
         const int w = (int)value;
-        if (w < -1 || w > WITHHOLD_QUANT) return fail(RMM_ERR_INVALID_ARG, "debug_control: withhold must be -1 .. %d", (int)WITHHOLD_QUANT);
+        if (w < -1 || w > WITHHOLD_KV4) return fail(RMM_ERR_INVALID_ARG, "debug_control: withhold must be -1 .. %d", (int)WITHHOLD_KV4);
         g_withhold_override.store(w, std::memory_order_relaxed);
         return RMM_OK;
     }

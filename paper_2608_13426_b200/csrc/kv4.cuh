@@ -1,0 +1,87 @@
+// A paged key/value cache held in 4 bits (internal).
+//
+// Values: 64 columns of one token and head share a step s and a least value m, both bf16:  x = m + s n,  n = 0 .. 15,
+//   m = min x,  s = bf16((max x - m) / 15),  n = min(15, round((x - m) / s))  (0 where s = 0; halves to the even code),
+// taken on bf16 numbers, so m is exact and every step of the rule is one IEEE fp32 operation.  4.5 bits a value.
+//
+// Layout: 16 tokens of one kv head are one block of 18 Dh contiguous bytes, so one bulk copy brings keys, values and steps of a
+// block.  The codes lie in the order in which the attention's matrix instructions want them, eight columns to a 32-bit word:
+//   words [0, 2 Dh)         keys: token t, columns 8 c .. 8 c + 7 at  t Dh/8 + (c % 4) Dh/32 + c / 4
+//                           (four lanes share a key, each with the words c = lane, lane + 4, ..: one wide load a lane)
+//   words [2 Dh, 4 Dh)      values: token t = 8 h + 2 q + e, columns 8 (8 j + g) ..: lane 4 g + q finds tokens e = 0, 1 and, where
+//                           heads are wide, j = 2 i, 2 i + 1 in neighbouring words
+//   words [4 Dh, 4.25 Dh)   keys' (s, m) pairs, s in the low half: token t, columns 64 j .. at  t Dh/64 + j
+//   words [4.25 Dh, 4.5 Dh) values' pairs
+#pragma once
+#include "heads.cuh"
+
+namespace rmm {
+namespace kv4 {
+
+constexpr int kBlock = 16;
+
+__host__ __device__ __forceinline__ int64_t block_bytes(int64_t D) { return 18 * D; }
+__device__ __forceinline__ int key_word(int D, int t, int c) { return t * (D / 8) + (c & 3) * (D / 32) + (c >> 2); }
+__device__ __forceinline__ int value_word(int D, int t, int c)
+{
+    const int h = t >> 3, q = (t >> 1) & 3, e = t & 1, g = c & 7, j = c >> 3, lane = 4 * g + q;
+    return 2 * D + (D == 64 ? (h * 32 + lane) * 2 + e : (((j >> 1) * 2 + h) * 32 + lane) * 4 + e * 2 + (j & 1));
+}
+__device__ __forceinline__ int key_pair_word(int D, int t, int j) { return 4 * D + t * (D / 64) + j; }
+__device__ __forceinline__ int value_pair_word(int D, int t, int j) { return 4 * D + D / 4 + t * (D / 64) + j; }
+
+// The cache as a kernel sees it.
+struct View {
+    uint8_t *pool;
+    int64_t page_stride, head_stride;   // bytes
+    const int32_t *pages;
+    int64_t pages_stride, max_pages, n_pages;
+    const int32_t *lengths, *new_len;   // new_len NULL: `rows` of every sequence
+    int page_shift;                     // log2 of the 16-token blocks of a page
+    int rows;
+};
+
+// Tokens a sequence holds, and how many of them are the call's rows; what the description does not allow is cut and reported.
+__device__ __forceinline__ void sequence(const View &v, int64_t b, int &len, int &rows, int *status)
+{
+    len = v.lengths[b];
+    rows = v.new_len != nullptr ? v.new_len[b] : v.rows;
+    const int64_t room = (v.max_pages << v.page_shift) * kBlock;
+    if (len < 0 || len > room || rows < 0 || rows > v.rows) {
+        atomicExch(status, (int)RMM_ERR_BOUNDS);
+        len = len < 0 ? 0 : (len > room ? (int)room : len);
+        rows = rows < 0 ? 0 : (rows > v.rows ? v.rows : rows);
+    }
+}
+
+// 16-token block t of a sequence's head, or NULL (reported) where its page is none of the pool's.
+__device__ __forceinline__ uint8_t *block_of(const View &v, int64_t b, int64_t head, int64_t t, int D, int *status)
+{
+    const int p = v.pages[b * v.pages_stride + (t >> v.page_shift)];
+    if (p < 0 || p >= v.n_pages) {
+        atomicExch(status, (int)RMM_ERR_BOUNDS);
+        return nullptr;
+    }
+    return v.pool + (int64_t)p * v.page_stride + head * v.head_stride + (t & ((1 << v.page_shift) - 1)) * block_bytes(D);
+}
+
+}  // namespace kv4
+
+int launch_kv4_append(const HeadRows &K, const HeadRows &V, const kv4::View &cache, int in_bf16, const RopeView &rope, int64_t B, int64_t L, int64_t D,
+                      int *status, cudaStream_t stream);
+int launch_kv4_read(const HeadRows &K, const HeadRows &V, const kv4::View &cache, int out_bf16, int64_t B, int64_t L, int64_t D, int *status,
+                    cudaStream_t stream);
+
+struct Kv4AttnProblem {
+    const void *q;
+    void *o;
+    int64_t q_sb, q_sh, q_sr, o_sb, o_sh, o_sr;
+    int64_t B, Hq, Hkv, L, D, kd;
+    int causal;
+    int32_t *idx_feat;
+};
+bool kv4_attn_fits(const Kv4AttnProblem &p, const kv4::View &cache);
+size_t kv4_attn_workspace_bytes(const Kv4AttnProblem &p);
+int launch_kv4_attn(const Kv4AttnProblem &p, const kv4::View &cache, float *scratch, unsigned *counters, int *status, cudaStream_t stream);
+
+}  // namespace rmm

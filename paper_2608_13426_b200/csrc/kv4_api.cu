@@ -1,0 +1,232 @@
+// C ABI of the operators on rows of heads and on the 4-bit cache: argument checks and dispatch (kernels: norm_rope.cu,
+// kv4_cache.cu, kv4_attn.cu).
+#include <math.h>
+
+#include "kv4.cuh"
+
+namespace rmm {
+namespace {
+
+int check_heads(const rmm_heads_t *x, const char *who, const char *name)
+{
+    if (x == nullptr || x->ptr == nullptr) return fail(RMM_ERR_INVALID_ARG, "%s: %s is NULL", who, name);
+    if (x->B < 1 || x->H < 1 || x->L < 1 || x->D < 1) return fail(RMM_ERR_INVALID_ARG, "%s: %s has a non-positive dimension", who, name);
+    if (x->dtype != RMM_BF16 && x->dtype != RMM_F32) return fail(RMM_ERR_UNSUPPORTED, "%s: %s must be bf16 or fp32", who, name);
+    if (x->stride[0] < 0 || x->stride[1] < 0 || x->stride[2] < 0) return fail(RMM_ERR_UNSUPPORTED, "%s: %s has a negative stride", who, name);
+    if (reinterpret_cast<uintptr_t>(x->ptr) % dtype_size(x->dtype) != 0) return fail(RMM_ERR_UNSUPPORTED, "%s: %s is misaligned", who, name);
+    if (x->B > INT32_MAX || x->H > INT32_MAX || x->L > INT32_MAX) return fail(RMM_ERR_UNSUPPORTED, "%s: %s has a dimension beyond 2^31", who, name);
+    return RMM_OK;
+}
+
+int check_same(const rmm_heads_t *x, const rmm_heads_t *y, const char *who, const char *name)
+{
+    if (x->B != y->B || x->H != y->H || x->L != y->L || x->D != y->D) return fail(RMM_ERR_INVALID_ARG, "%s: the shape of %s disagrees", who, name);
+    return RMM_OK;
+}
+
+int check_rope(const rmm_rope_t *r, int64_t D, const void *weight, const char *who)
+{
+    if (weight != nullptr && r == nullptr) return fail(RMM_ERR_INVALID_ARG, "%s: a norm needs a description (weight type and eps)", who);
+    if (r == nullptr) return RMM_OK;
+    if (weight != nullptr) {
+        if (r->weight_dtype != RMM_BF16 && r->weight_dtype != RMM_F32) return fail(RMM_ERR_UNSUPPORTED, "%s: weights must be bf16 or fp32", who);
+        if (reinterpret_cast<uintptr_t>(weight) % dtype_size(r->weight_dtype) != 0) return fail(RMM_ERR_UNSUPPORTED, "%s: weights are misaligned", who);
+        if (!(r->eps >= 0.0) || !(r->eps <= 1e30)) return fail(RMM_ERR_INVALID_ARG, "%s: eps must be finite and not negative", who);
+    }
+    if (r->table == nullptr) return RMM_OK;
+    if (r->rot < 2 || r->rot > D) return fail(RMM_ERR_INVALID_ARG, "%s: rot = %lld is outside [2, %lld]", who, (long long)r->rot, (long long)D);
+    if (r->rot % 16 != 0) return fail(RMM_ERR_UNSUPPORTED, "%s: rot = %lld is no multiple of 16", who, (long long)r->rot);
+    if (r->table_rows < 1 || r->table_stride < r->rot) return fail(RMM_ERR_INVALID_ARG, "%s: the table's rows are shorter than rot, or there are none", who);
+    if (reinterpret_cast<uintptr_t>(r->table) % 4 != 0) return fail(RMM_ERR_UNSUPPORTED, "%s: the table is misaligned", who);
+    if (r->positions != nullptr && (r->pos_stride[0] < 0 || r->pos_stride[1] < 0 || reinterpret_cast<uintptr_t>(r->positions) % 4 != 0))
+        return fail(RMM_ERR_UNSUPPORTED, "%s: positions are misaligned or have a negative stride", who);
+    return RMM_OK;
+}
+
+int check_cache(const rmm_kv4_t *c, int64_t B, const char *who)
+{
+    if (c == nullptr || c->pool == nullptr || c->pages == nullptr || c->lengths == nullptr) return fail(RMM_ERR_INVALID_ARG, "%s: the cache has a NULL pointer", who);
+    if (c->Dh != 64 && c->Dh != 128 && c->Dh != 256) return fail(RMM_ERR_UNSUPPORTED, "%s: cached heads have 64, 128 or 256 columns, not %lld", who, (long long)c->Dh);
+    if (c->n_pages < 1 || c->Hkv < 1 || c->B < 1 || c->max_pages < 1) return fail(RMM_ERR_INVALID_ARG, "%s: the cache has a non-positive dimension", who);
+    if (c->B != B) return fail(RMM_ERR_INVALID_ARG, "%s: the cache describes %lld sequences, not %lld", who, (long long)c->B, (long long)B);
+    if (c->page < 16 || c->page > (1 << 20) || (c->page & (c->page - 1)) != 0) return fail(RMM_ERR_UNSUPPORTED, "%s: page = %lld is no power of two from 16 on", who, (long long)c->page);
+    const int64_t head = c->page / kv4::kBlock * kv4::block_bytes(c->Dh);
+    if (reinterpret_cast<uintptr_t>(c->pool) % 16 != 0 || c->page_stride % 16 != 0 || c->head_stride % 16 != 0)
+        return fail(RMM_ERR_UNSUPPORTED, "%s: the pool and its strides must be multiples of 16 bytes", who);
+    if ((c->head_stride < head && c->Hkv > 1) || (c->page_stride < head && c->n_pages > 1))
+        return fail(RMM_ERR_INVALID_ARG, "%s: the pool's strides overlap (a head's page takes %lld bytes)", who, (long long)head);
+    if (c->pages_stride < 0 || c->max_pages > INT32_MAX / c->page || c->n_pages > INT32_MAX) return fail(RMM_ERR_UNSUPPORTED, "%s: sequences beyond 2^31 tokens, or a negative stride", who);
+    if (reinterpret_cast<uintptr_t>(c->pages) % 4 != 0 || reinterpret_cast<uintptr_t>(c->lengths) % 4 != 0 || reinterpret_cast<uintptr_t>(c->new_len) % 4 != 0)
+        return fail(RMM_ERR_UNSUPPORTED, "%s: pages, lengths or new_len are misaligned", who);
+    return RMM_OK;
+}
+
+int check_ws(void *ws, size_t have, size_t need, const char *who)
+{
+    if (ws == nullptr || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || have < need)
+        return fail(RMM_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned and hold %zu bytes", who, need);
+    return RMM_OK;
+}
+
+int vectors(const rmm_heads_t *x)
+{
+    const size_t size = dtype_size(x->dtype);
+    return reinterpret_cast<uintptr_t>(x->ptr) % 16 == 0 && x->stride[0] * size % 16 == 0 && x->stride[1] * size % 16 == 0 && x->stride[2] * size % 16 == 0;
+}
+
+HeadRows rows_of(const rmm_heads_t *x, const rmm_heads_t *y, const void *weight)
+{
+    HeadRows r = {};
+    r.weight = weight;
+    if (x != nullptr) {
+        r.src = x->ptr;
+        r.s_b = x->stride[0]; r.s_h = x->stride[1]; r.s_r = x->stride[2];
+        r.heads = (int)x->H;
+        r.vec_in = vectors(x);
+    }
+    if (y != nullptr) {
+        r.dst = y->ptr;
+        r.d_b = y->stride[0]; r.d_h = y->stride[1]; r.d_r = y->stride[2];
+        r.heads = (int)y->H;
+        r.vec_out = vectors(y);
+    }
+    return r;
+}
+
+RopeView rope_of(const rmm_rope_t *r)
+{
+    RopeView v = {};
+    if (r == nullptr) return v;
+    v.table = r->table;
+    v.rows = r->table_rows;
+    v.stride = r->table_stride;
+    v.positions = r->positions;
+    v.p_b = r->pos_stride[0];
+    v.p_r = r->pos_stride[1];
+    v.rot = r->table != nullptr ? (int)r->rot : 0;
+    v.interleaved = r->interleaved;
+    v.weight_bf16 = r->weight_dtype == RMM_BF16;
+    v.eps = (float)r->eps;
+    return v;
+}
+
+kv4::View view_of(const rmm_kv4_t *c, int64_t L)
+{
+    kv4::View v = {};
+    v.pool = static_cast<uint8_t *>(c->pool);
+    v.page_stride = c->page_stride;
+    v.head_stride = c->head_stride;
+    v.pages = c->pages;
+    v.pages_stride = c->pages_stride;
+    v.max_pages = c->max_pages;
+    v.n_pages = c->n_pages;
+    v.lengths = c->lengths;
+    v.new_len = c->new_len;
+    for (int64_t p = c->page / kv4::kBlock; p > 1; p /= 2) ++v.page_shift;
+    v.rows = (int)L;
+    return v;
+}
+
+int plan_kv4_attn(const rmm_heads_t *Q, const rmm_kv4_t *cache, Kv4AttnProblem *p, const char *who)
+{
+    int rc;
+    if ((rc = check_heads(Q, who, "Q")) || (rc = check_cache(cache, Q->B, who))) return rc;
+    if (Q->dtype != RMM_BF16) return fail(RMM_ERR_UNSUPPORTED, "%s: Q must be bf16", who);
+    if (Q->D != cache->Dh || Q->H % cache->Hkv != 0) return fail(RMM_ERR_INVALID_ARG, "%s: the cache has other columns than Q, or heads that Q's are no multiple of", who);
+    *p = Kv4AttnProblem{};
+    p->q = Q->ptr;
+    p->q_sb = Q->stride[0]; p->q_sh = Q->stride[1]; p->q_sr = Q->stride[2];
+    p->B = Q->B; p->Hq = Q->H; p->Hkv = cache->Hkv; p->L = Q->L; p->D = Q->D;
+    if (!kv4_attn_fits(*p, view_of(cache, Q->L))) return fail(RMM_ERR_UNSUPPORTED, "%s: more than 2^31 blocks of keys over all row tiles", who);
+    return RMM_OK;
+}
+
+}  // namespace
+}  // namespace rmm
+
+using namespace rmm;
+
+extern "C" {
+
+int rmm_qk_norm_rope(const rmm_heads_t *Q, const rmm_heads_t *K, const void *q_weight, const void *k_weight, const rmm_rope_t *rope,
+                     const rmm_heads_t *Q_out, const rmm_heads_t *K_out, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "qk_norm_rope";
+    int rc;
+    if ((rc = check_heads(Q, who, "Q")) || (rc = check_heads(Q_out, who, "Q_out")) || (rc = check_same(Q, Q_out, who, "Q_out"))) return rc;
+    if ((K == nullptr) != (K_out == nullptr)) return fail(RMM_ERR_INVALID_ARG, "%s: K and K_out come together", who);
+    if (K != nullptr) {
+        if ((rc = check_heads(K, who, "K")) || (rc = check_heads(K_out, who, "K_out")) || (rc = check_same(K, K_out, who, "K_out"))) return rc;
+        if (K->B != Q->B || K->L != Q->L || K->D != Q->D) return fail(RMM_ERR_INVALID_ARG, "%s: Q and K have different sequences, rows or columns", who);
+        if (K->dtype != Q->dtype || K_out->dtype != Q_out->dtype) return fail(RMM_ERR_UNSUPPORTED, "%s: Q and K must share a dtype", who);
+    }
+    if (Q->D % 8 != 0 || Q->D > 256) return fail(RMM_ERR_UNSUPPORTED, "%s: heads have a multiple of 8 columns up to 256, not %lld", who, (long long)Q->D);
+    if ((rc = check_rope(rope, Q->D, q_weight, who)) || (K != nullptr && (rc = check_rope(rope, Q->D, k_weight, who)))) return rc;
+    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who))) return rc;
+    const HeadRows rows[2] = {rows_of(Q, Q_out, q_weight), rows_of(K, K_out, K != nullptr ? k_weight : nullptr)};
+    return launch_norm_rope(rows, Q->dtype == RMM_BF16, Q_out->dtype == RMM_BF16, rope_of(rope), Q->B, Q->L, Q->D,
+                            &static_cast<WsHeader *>(ws)->status, static_cast<cudaStream_t>(stream));
+}
+
+int rmm_kv4_append(const rmm_heads_t *K, const rmm_heads_t *V, const rmm_kv4_t *cache, const void *k_weight, const rmm_rope_t *rope,
+                   const rmm_heads_t *K_held, const rmm_heads_t *V_held, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "kv4_append";
+    int rc;
+    if ((rc = check_heads(K, who, "K")) || (rc = check_heads(V, who, "V")) || (rc = check_same(K, V, who, "V"))) return rc;
+    if (K->dtype != V->dtype) return fail(RMM_ERR_UNSUPPORTED, "%s: K and V must share a dtype", who);
+    if ((rc = check_cache(cache, K->B, who))) return rc;
+    if (K->H != cache->Hkv || K->D != cache->Dh) return fail(RMM_ERR_INVALID_ARG, "%s: the cache has other heads than K", who);
+    if ((K_held == nullptr) != (V_held == nullptr)) return fail(RMM_ERR_INVALID_ARG, "%s: K_held and V_held come together", who);
+    if (K_held != nullptr) {
+        if ((rc = check_heads(K_held, who, "K_held")) || (rc = check_heads(V_held, who, "V_held")) || (rc = check_same(K, K_held, who, "K_held")) ||
+            (rc = check_same(K, V_held, who, "V_held")))
+            return rc;
+        if (K_held->dtype != RMM_BF16 || V_held->dtype != RMM_BF16) return fail(RMM_ERR_UNSUPPORTED, "%s: held values are bf16", who);
+    }
+    if ((rc = check_rope(rope, K->D, k_weight, who)) || (rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who))) return rc;
+    return launch_kv4_append(rows_of(K, K_held, k_weight), rows_of(V, V_held, nullptr), view_of(cache, K->L), K->dtype == RMM_BF16, rope_of(rope), K->B,
+                             K->L, K->D, &static_cast<WsHeader *>(ws)->status, static_cast<cudaStream_t>(stream));
+}
+
+int rmm_kv4_read(const rmm_kv4_t *cache, const rmm_heads_t *K, const rmm_heads_t *V, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "kv4_read";
+    int rc;
+    if ((rc = check_heads(K, who, "K")) || (rc = check_heads(V, who, "V")) || (rc = check_same(K, V, who, "V"))) return rc;
+    if (K->dtype != V->dtype) return fail(RMM_ERR_UNSUPPORTED, "%s: K and V must share a dtype", who);
+    if ((rc = check_cache(cache, K->B, who))) return rc;
+    if (K->H != cache->Hkv || K->D != cache->Dh) return fail(RMM_ERR_INVALID_ARG, "%s: the cache has other heads than K", who);
+    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who))) return rc;
+    return launch_kv4_read(rows_of(nullptr, K, nullptr), rows_of(nullptr, V, nullptr), view_of(cache, K->L), K->dtype == RMM_BF16, K->B, K->L, K->D,
+                           &static_cast<WsHeader *>(ws)->status, static_cast<cudaStream_t>(stream));
+}
+
+size_t rmm_kv4_attn_workspace_bytes(const rmm_heads_t *Q, const rmm_kv4_t *cache)
+{
+    Kv4AttnProblem p;
+    return plan_kv4_attn(Q, cache, &p, "kv4_attn") != RMM_OK ? 0 : RMM_WS_HEADER_BYTES + kv4_attn_workspace_bytes(p);
+}
+
+int rmm_kv4_attn(const rmm_heads_t *Q, const rmm_kv4_t *cache, int causal, double rho_d, const rmm_heads_t *O, int32_t *idx_feat,
+                 void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "kv4_attn";
+    Kv4AttnProblem p;
+    int rc;
+    if ((rc = plan_kv4_attn(Q, cache, &p, who))) return rc;
+    if ((rc = check_heads(O, who, "O")) || (rc = check_same(Q, O, who, "O"))) return rc;
+    if (O->dtype != RMM_BF16) return fail(RMM_ERR_UNSUPPORTED, "%s: O must be bf16", who);
+    if (rmm_keep_count(rho_d, p.D, &p.kd) != RMM_OK) return fail(RMM_ERR_INVALID_ARG, "%s: rho_d = %g is outside (0, 1]", who, rho_d);
+    if ((p.kd < p.D || idx_feat != nullptr) && p.L > kDecodeMaxRows) return fail(RMM_ERR_UNSUPPORTED, "%s: features are selected for up to %d rows", who, (int)kDecodeMaxRows);
+    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES + kv4_attn_workspace_bytes(p), who))) return rc;
+    p.o = O->ptr;
+    p.o_sb = O->stride[0]; p.o_sh = O->stride[1]; p.o_sr = O->stride[2];
+    p.causal = causal != 0;
+    p.idx_feat = idx_feat;
+    WsHeader *h = static_cast<WsHeader *>(ws);
+    return launch_kv4_attn(p, view_of(cache, Q->L), reinterpret_cast<float *>(static_cast<char *>(ws) + RMM_WS_HEADER_BYTES), h->counters, &h->status,
+                           static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
