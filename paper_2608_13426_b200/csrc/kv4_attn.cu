@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                 ml[(w * ROWS + tid) * 2] = f;
             }
             tot[tid * 2] = mx;
-            tot[tid * 2 + 1] = sum;
+            tot[tid * 2 + 1] = tid < nrows ? sum : 0.f;   // (rows that are none have met keys all the same)
         }
         float *part = nullptr;
         if (!whole) part = a.part + (int64_t)(2 * blockIdx.x + (t_at == 0 ? 1 : 0)) * ROWS * (D + 2);
