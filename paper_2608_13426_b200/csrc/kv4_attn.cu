@@ -13,13 +13,16 @@
 //     2^-25 against a largest weight of 2^6.
 //   - S^T = K Q^T and O^T = V^T P^T, so that the 8 columns of an instruction are query rows that share a kv head and its 16 rows are
 //     keys (or columns of V): the group's rows fill what 128-row tcgen05 tiles would pad.
-// The 16-token blocks of all jobs (sequence, kv head, row tile) form one axis that is cut into equal shares, one a CTA, whatever the
-// lengths are: they live on the device, so nothing is planned on the host and a captured call follows them.  Within a CTA every
-// warp takes every eighth block through a ring of its own, filled by bulk copies of whole blocks, which runs on across jobs.  A job
-// that ends in another CTA leaves its sums in the workspace; the last CTA of a job to arrive adds them up, in order.
+// The pairs of 16-token blocks of all jobs (sequence, kv head, row tile) form one axis that is cut into equal shares, one a CTA, whatever
+// the lengths are: they live on the device, so nothing is planned on the host and a captured call follows them.  A job counts kFixed
+// pairs more than it has, for what a CTA spends on it outside the keys.  Within a CTA every warp takes every fourth pair through a
+// ring of its own, filled by bulk copies of whole blocks, which runs on across jobs.  A job that ends in another CTA leaves its sums in
+// the workspace; the last CTA of a job to arrive adds them up, in order.
 #include <math.h>
 
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "kv4.cuh"
 #include "select.cuh"
@@ -28,17 +31,20 @@
 namespace rmm {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr float kGrow = 14.f, kTop = 6.f, kLeastStep = -80.f;   // log2: see above; steps below 2^-80 weigh as 2^-80 in the reference
+constexpr int kWarps = 4, kPair = 2 * kv4::kBlock;   // warps of a CTA; tokens of a warp's turn
+constexpr int kFixed = 12, kLeast = kFixed + 16;     // pairs that a job's fixed part counts as; the least share of a CTA
+constexpr float kTopWeight = 16384.f, kTop = 6.f, kLeastStep = 8.2718061e-25f;   // 2^14, log2 of 2^6, 2^-80: see above; smaller steps weigh as that
+constexpr float kNone = 1e30f;                       // minus the reference of a row that has seen no key
 
 struct AttnArgs {
     const __nv_bfloat16 *q;
     __nv_bfloat16 *o;
     int64_t q_sb, q_sh, q_sr, o_sb, o_sh, o_sr;
     kv4::View cache;
-    int B, Hkv, group, L, kd, causal, chunks;
+    int B, Hkv, group, L, kd, chunks;
+    int causal;
     float scale_log2;
-    int32_t *idx_feat;
+    const uint32_t *kept;     // [B][Hq][D / 32] bit masks of the kept features, or NULL: all
     float *part;              // [2 CTAs][rows][D + 2]: sums, then (reference, sum of weights)
     unsigned *counters;
     int *status;
@@ -48,21 +54,19 @@ struct AttnArgs {
 
 template <int D, int NT>
 struct Shape {
-    static constexpr int kRows = 8 * NT, kBlockBytes = 18 * D, kGroups = D / 64;
-    static constexpr int kCtas = D * NT <= 128 ? 2 : 1;                        // an SM
-    static constexpr int kStages = D == 64 ? 8 : (D == 128 ? (NT == 1 ? 4 : 8) : 4);
-    static constexpr int kPitchQ = D + 8, kPitchM = 66;
-    static constexpr int kOffQ = kWarps * kStages * kBlockBytes;               // fp16 [rows][pitch]
-    static constexpr int kOffMerge = kOffQ + kRows * kPitchQ * 2;              // fp32 [warp][row][pitch]
+    static constexpr int kRows = 8 * NT, kBlockBytes = 18 * D, kPairBytes = 2 * kBlockBytes, kGroups = D / 64;
+    static constexpr int kCtas = D * NT <= 128 ? 4 : 2;                        // an SM
+    static constexpr int kStages = D == 64 ? 4 : (D == 128 && NT == 2 ? 4 : 2);
+    static constexpr int kPitchM = 66;
+    static constexpr int kOffQ = kWarps * kStages * kPairBytes;                // fp16 fragments [row tile of 8][D / 32][lane][4 words]
+    static constexpr int kOffMerge = kOffQ + kRows * D * 2;                    // fp32 [warp][row][pitch]
     static constexpr int kOffMl = kOffMerge + kWarps * kRows * kPitchM * 4;    // [warp][row]: (reference, sum), then the warp's factor
     static constexpr int kOffRow = kOffMl + kWarps * kRows * 8;                // [row]: scale, visible keys, then sums of q by group
-    static constexpr int kOffKept = kOffRow + kRows * (2 + kGroups) * 4;       // [row's head][D / 32]
-    static constexpr int kOffTot = kOffKept + kRows * (D / 32) * 4;            // [row]: reference, sum of the CTA
+    static constexpr int kOffTot = kOffRow + kRows * (2 + kGroups) * 4;        // [row]: reference, sum of the CTA
     static constexpr int kOffBar = (kOffTot + kRows * 8 + 15) / 16 * 16;       // barriers, then the tokens of each ring entry
     static constexpr int kSmem = kOffBar + kWarps * kStages * 12;
-    static_assert(kSmem <= 227 * 1024 / kCtas - 2048, "shared memory");
+    static_assert(kSmem <= 227 * 1024 / kCtas - 1280, "shared memory");
 };
-
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -82,86 +86,95 @@ __device__ __forceinline__ float lg2(float x)
     return y;
 }
 
-// A place on the axis of all jobs' blocks.
-struct Cursor {
-    int b, len, rows, nb, valid;   // sequence, its tokens and rows, blocks of a job, row tiles that hold rows
+// A job on the axis of all jobs' pairs.
+struct Job {
+    int b, len, rows, nb, valid;   // sequence, its tokens and rows, pairs of a reading job, row tiles that hold rows
     int hk, chunk;
-    __device__ __forceinline__ int blocks() const { return chunk < valid ? nb : 1; }
     __device__ __forceinline__ bool reads() const { return chunk < valid && len > 0; }
+    __device__ __forceinline__ int cost() const { return reads() ? nb + kFixed : 1; }
 };
 
 template <int ROWS>
-__device__ __forceinline__ void cursor_sequence(const AttnArgs &a, Cursor &c)
+__device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c)
 {
     kv4::sequence(a.cache, c.b, c.len, c.rows, a.status);
-    c.nb = max(1, (c.len + kv4::kBlock - 1) / kv4::kBlock);
+    c.nb = (c.len + kPair - 1) / kPair;
     c.valid = (c.rows * a.group + ROWS - 1) / ROWS;
 }
-template <int ROWS>
-__device__ __forceinline__ int sequence_units(const AttnArgs &a, int b)
+__device__ __forceinline__ int head_cost(const AttnArgs &a, const Job &c)
 {
-    Cursor c;
-    c.b = b;
-    cursor_sequence<ROWS>(a, c);
-    return a.Hkv * (c.valid * c.nb + a.chunks - c.valid);
+    return c.len > 0 ? c.valid * (c.nb + kFixed) + a.chunks - c.valid : a.chunks;
 }
 template <int ROWS>
-__device__ __forceinline__ void cursor_next(const AttnArgs &a, Cursor &c)
+__device__ __forceinline__ int sequence_cost(const AttnArgs &a, int b)
+{
+    Job c;
+    c.b = b;
+    job_sequence<ROWS>(a, c);
+    return a.Hkv * head_cost(a, c);
+}
+template <int ROWS>
+__device__ __forceinline__ void job_next(const AttnArgs &a, Job &c)
 {
     if (++c.chunk < a.chunks) return;
     c.chunk = 0;
     if (++c.hk < a.Hkv) return;
     c.hk = 0;
-    if (++c.b < a.B) cursor_sequence<ROWS>(a, c);
+    if (++c.b < a.B) job_sequence<ROWS>(a, c);
 }
 
-// Kept features of the heads of a row tile (one warp a head) as bit masks; the rule of every other form: squares summed in fp64,
-// rounded to fp32, the kd largest, the lower index first.
-template <int D>
-__device__ __noinline__ void keep_features(const AttnArgs &a, int b, int hk, int rows, int row0, int nrows, bool first, uint32_t *kept)
+// Kept features of one head a warp, as bit masks; the rule of every other form: squares summed in fp64, rounded to fp32, the kd
+// largest, the lower index first.
+template <int W32>
+__global__ void __launch_bounds__(128) kv4_features_kernel(const __grid_constant__ AttnArgs a, uint32_t *kept, int32_t *idx_feat)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int idx = warp; idx < min(a.group, nrows); idx += kWarps) {
-        const int64_t h = (int64_t)hk * a.group + (row0 + idx) % a.group;
-        const __nv_bfloat16 *qp = a.q + b * a.q_sb + h * a.q_sh;
-        uint32_t u[D / 32];
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t job = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), Hq = (int64_t)a.Hkv * a.group;
+    if (job >= a.B * Hq) return;
+    const int64_t b = job / Hq, h = job - b * Hq;
+    int len, rows;
+    kv4::sequence(a.cache, b, len, rows, a.status);
+    const __nv_bfloat16 *qp = a.q + b * a.q_sb + h * a.q_sh + lane;
+    double e[W32];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            double e = 0.0;
-            for (int r = 0; r < rows; ++r) {
-                const float x = __bfloat162float(qp[r * a.q_sr + i * 32 + lane]);
-                e += (double)(x * x);
-            }
-            u[i] = sel::key_image((float)e);
+    for (int i = 0; i < W32; ++i) e[i] = 0.0;
+    for (int r = 0; r < rows; ++r)
+#pragma unroll
+        for (int i = 0; i < W32; ++i) {
+            const float x = __bfloat162float(qp[r * a.q_sr + i * 32]);
+            e[i] += (double)(x * x);
         }
-        uint32_t tau = 0;
+    uint32_t u[W32];
+#pragma unroll
+    for (int i = 0; i < W32; ++i) u[i] = sel::key_image((float)e[i]);
+    uint32_t tau = 0;   // largest value that at least kd keys reach
 #pragma unroll 1
-        for (int bit = 30; bit >= 0; bit -= 2) {
-            int n[3] = {0, 0, 0};
+    for (int bit = 30; bit >= 0; bit -= 2) {
+        int n[3] = {0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i)
+        for (int i = 0; i < W32; ++i)
 #pragma unroll
-                for (int v = 0; v < 3; ++v) n[v] += u[i] >= (tau | ((unsigned)(v + 1) << bit)) ? 1 : 0;
-            unsigned digit = 0;
+            for (int v = 0; v < 3; ++v) n[v] += u[i] >= (tau | ((unsigned)(v + 1) << bit)) ? 1 : 0;
+        unsigned digit = 0;
 #pragma unroll
-            for (int v = 0; v < 3; ++v) digit += __reduce_add_sync(0xffffffffu, n[v]) >= a.kd ? 1u : 0u;
-            tau |= digit << bit;
-        }
-        int n = 0;
+        for (int v = 0; v < 3; ++v) digit += __reduce_add_sync(0xffffffffu, n[v]) >= a.kd ? 1u : 0u;
+        tau |= digit << bit;
+    }
+    int n = 0;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) n += u[i] > tau ? 1 : 0;
-        int need = a.kd - __reduce_add_sync(0xffffffffu, n), at = 0;
-        int32_t *out = first && a.idx_feat != nullptr && row0 + idx < a.group ? a.idx_feat + ((int64_t)b * a.Hkv * a.group + h) * a.kd : nullptr;
+    for (int i = 0; i < W32; ++i) n += u[i] > tau ? 1 : 0;
+    int need = a.kd - __reduce_add_sync(0xffffffffu, n), at = 0;
+    int32_t *out = idx_feat != nullptr && rows > 0 ? idx_feat + job * a.kd : nullptr;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            const unsigned eq = __ballot_sync(0xffffffffu, u[i] == tau), lt = (1u << lane) - 1u;
-            const bool keep = u[i] > tau || (u[i] == tau && __popc(eq & lt) < need);
-            need -= min(need, __popc(eq));
-            const unsigned m = __ballot_sync(0xffffffffu, keep);
-            if (out != nullptr && keep) out[at + __popc(m & lt)] = i * 32 + lane;
-            at += __popc(m);
-            if (lane == 0) kept[idx * (D / 32) + i] = m;
-        }
+    for (int i = 0; i < W32; ++i) {
+        const unsigned eq = __ballot_sync(0xffffffffu, u[i] == tau), lt = (1u << lane) - 1u;
+        const bool keep = u[i] > tau || (u[i] == tau && __popc(eq & lt) < need);
+        need -= min(need, __popc(eq));
+        const unsigned m = __ballot_sync(0xffffffffu, keep);
+        if (out != nullptr && keep) out[at + __popc(m & lt)] = i * 32 + lane;
+        at += __popc(m);
+        if (lane == 0) kept[job * W32 + i] = m;
     }
 }
 
@@ -170,17 +183,16 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
 {
     using namespace ptx;
     using S = Shape<D, NT>;
-    constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32;
+    constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32, THREADS = kWarps * 32;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int s_scan[kWarps], s_begin[2], abort_flag, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = smem_u32(smem) + warp * ST * S::kBlockBytes, bars = smem_u32(smem) + S::kOffBar + warp * ST * 8;
-    int *tokens = reinterpret_cast<int *>(smem + S::kOffBar + kWarps * ST * 8) + warp * ST;
+    const uint32_t ring = smem_u32(smem) + warp * ST * S::kPairBytes, bars = smem_u32(smem) + S::kOffBar + warp * ST * 8;
+    int *tokens = reinterpret_cast<int *>(smem + S::kOffBar + kWarps * ST * 8) + warp * ST;   // of the first block, + 256 x of the second
     __half *qs = reinterpret_cast<__half *>(smem + S::kOffQ);
     float *merge = reinterpret_cast<float *>(smem + S::kOffMerge), *ml = reinterpret_cast<float *>(smem + S::kOffMl);
     float *row_scale = reinterpret_cast<float *>(smem + S::kOffRow), *row_sum = row_scale + 2 * ROWS, *tot = reinterpret_cast<float *>(smem + S::kOffTot);
     int *row_vis = reinterpret_cast<int *>(row_scale + ROWS);
-    uint32_t *kept = reinterpret_cast<uint32_t *>(smem + S::kOffKept);
 
     if (lane == 0)
         for (int i = 0; i < ST; ++i) mbar_init(bars + 8 * i, 1);
@@ -209,426 +221,476 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         return v + before;
     };
     int total = 0, mine = 0, upto = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWarps * 32) {
+    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         int sum;
-        mine = b0 + tid < a.B ? sequence_units<ROWS>(a, b0 + tid) : 0;
+        mine = b0 + tid < a.B ? sequence_cost<ROWS>(a, b0 + tid) : 0;
         upto = scan(mine, sum);
         total += sum;
     }
-    const int ctas = min((int)gridDim.x, (total + kWarps - 1) / kWarps);   // eight blocks each at least
+    const int ctas = min((int)gridDim.x, (total + kLeast - 1) / kLeast);
     if ((int)blockIdx.x >= ctas) return;
-    int u = (int)((int64_t)total * blockIdx.x / ctas);
-    const int u_end = (int)((int64_t)total * (blockIdx.x + 1) / ctas);
-    for (int b0 = 0, base = 0; b0 < a.B; b0 += kWarps * 32) {
+    const int u_begin = (int)((int64_t)total * blockIdx.x / ctas), u_end = (int)((int64_t)total * (blockIdx.x + 1) / ctas);
+    for (int b0 = 0, base = 0; b0 < a.B; b0 += THREADS) {
         int sum = 0;
-        if (a.B > kWarps * 32) {
-            mine = b0 + tid < a.B ? sequence_units<ROWS>(a, b0 + tid) : 0;
+        if (a.B > THREADS) {
+            mine = b0 + tid < a.B ? sequence_cost<ROWS>(a, b0 + tid) : 0;
             upto = scan(mine, sum);
         }
-        if (u >= base + upto - mine && u < base + upto) {
+        if (u_begin >= base + upto - mine && u_begin < base + upto) {
             s_begin[0] = b0 + tid;
-            s_begin[1] = u - (base + upto - mine);
+            s_begin[1] = base + upto - mine;
         }
         base += sum;
     }
     __syncthreads();
 
-    Cursor cur;
+    Job cur;
+    int start;   // where the current job begins on the axis
     cur.b = s_begin[0];
-    cursor_sequence<ROWS>(a, cur);
-    int t_at;   // first block of the current job's part
+    start = s_begin[1];
+    job_sequence<ROWS>(a, cur);
     {
-        const int per_head = cur.valid * cur.nb + a.chunks - cur.valid;
-        int off = s_begin[1];
+        const int per_head = head_cost(a, cur), each = cur.len > 0 ? cur.nb + kFixed : 1;
+        int off = u_begin - start;
         cur.hk = off / per_head;
         off -= cur.hk * per_head;
-        if (off < cur.valid * cur.nb) {
-            cur.chunk = off / cur.nb;
-            t_at = off - cur.chunk * cur.nb;
-        } else {
-            cur.chunk = cur.valid + off - cur.valid * cur.nb;
-            t_at = 0;
-        }
+        cur.chunk = off < cur.valid * each ? off / each : cur.valid + off - cur.valid * each;
+        start = u_begin - (off < cur.valid * each ? off - cur.chunk * each : 0);
     }
+    // the pairs of the job at `at` that are this CTA's
+    auto first_pair = [&](int at) { return max(0, u_begin - at - kFixed); };
+    auto last_pair = [&](const Job &c, int at) { return min(c.nb, u_end - at - kFixed); };
 
-    // ---- the warp's loads: blocks t_at + warp, + 8, .. of every part, ST of them under way
-    Cursor pc = cur;
-    int p_u = u, p_t0 = t_at, p_t = t_at + warp, p_page = 0, p_slot = 0;   // p_u: axis position of p_t0
-    auto settle = [&]() {   // on to the next block that has something to load; its page number is fetched here, ahead of its use
-        while (p_u < u_end) {
-            const int end = min(pc.blocks(), p_t0 + u_end - p_u);
-            if (pc.reads() && p_t < end) {
-                p_page = __ldg(a.cache.pages + pc.b * a.cache.pages_stride + (p_t >> a.cache.page_shift));
-                return;
+    // ---- the warp's loads: pairs first + warp, + 4, .. of every part, ST of them under way
+    Job pc = cur;
+    int p_start = start, p_t = 0, p_end = 0, p_k = 32, p_slot = 0, page0 = 0, page1 = 0;   // lanes hold the pages of the next 32 pairs
+    const bool split = a.cache.page_shift == 0;   // the blocks of a pair lie in two pages
+    auto settle = [&](bool next) {   // on to the next pair that has something to load
+        if (!next && p_t < p_end && p_k < 32) return;
+        while (true) {
+            if (next) {
+                p_start += pc.cost();
+                if (p_start >= u_end) {
+                    p_t = p_end = 0;
+                    return;
+                }
+                job_next<ROWS>(a, pc);
             }
-            p_u += end - p_t0;
-            p_t0 = 0;
-            p_t = warp;
-            if (p_u < u_end) cursor_next<ROWS>(a, pc);
+            if (next || p_k == 64) {
+                p_end = pc.reads() ? last_pair(pc, p_start) : 0;
+                p_t = first_pair(p_start) + warp;
+                p_k = 32;
+            }
+            if (p_t < p_end) break;
+            next = true;
+        }
+        if (p_k == 32) {
+            const int32_t *row = a.cache.pages + pc.b * a.cache.pages_stride;
+            const int t = 2 * (p_t + lane * kWarps), blocks = (pc.len + kv4::kBlock - 1) / kv4::kBlock;   // first block of the lane's pair
+            page0 = t < blocks ? __ldg(row + (t >> a.cache.page_shift)) : 0;
+            page1 = split && t + 1 < blocks ? __ldg(row + t + 1) : page0;
+            p_k = 0;
         }
     };
     auto request = [&]() {
-        if (p_u >= u_end) return;
+        if (p_t >= p_end) return;
+        const int i0 = __shfl_sync(0xffffffffu, page0, p_k), i1 = __shfl_sync(0xffffffffu, page1, p_k);
         if (lane == 0) {
-            const uint32_t bar = bars + 8 * p_slot;
-            const bool good = p_page >= 0 && p_page < a.cache.n_pages;
-            tokens[p_slot] = good ? min(kv4::kBlock, pc.len - p_t * kv4::kBlock) : 0;
-            if (!good) {
-                atomicExch(a.status, (int)RMM_ERR_BOUNDS);
-                mbar_arrive(bar);
-            } else if (!(a.withhold && blockIdx.x == 0 && warp == 0)) {   // (test switch: these copies are never requested)
-                const uint8_t *src = a.cache.pool + (int64_t)p_page * a.cache.page_stride + pc.hk * a.cache.head_stride +
-                                     (int64_t)(p_t & ((1 << a.cache.page_shift) - 1)) * S::kBlockBytes;
-                mbar_arrive_expect_tx(bar, S::kBlockBytes);
+            const uint32_t bar = bars + 8 * p_slot, dst = ring + (uint32_t)p_slot * S::kPairBytes;
+            const int left = pc.len - p_t * kPair;
+            const bool good0 = i0 >= 0 && i0 < a.cache.n_pages, good1 = i1 >= 0 && i1 < a.cache.n_pages;
+            int n0 = min(left, kv4::kBlock), n1 = max(0, min(left - kv4::kBlock, kv4::kBlock));
+            if (!good0 || (n1 > 0 && !good1)) atomicExch(a.status, (int)RMM_ERR_BOUNDS);
+            if (!good0) n0 = 0;
+            if (!good1) n1 = 0;
+            tokens[p_slot] = n0 | n1 << 8;
+            const uint32_t bytes = (n0 > 0 ? S::kBlockBytes : 0) + (n1 > 0 ? S::kBlockBytes : 0);
+            const uint8_t *src = a.cache.pool + pc.hk * a.cache.head_stride +
+                                 (int64_t)((2 * p_t) & ((1 << a.cache.page_shift) - 1)) * S::kBlockBytes;
+            auto copy = [&](uint32_t to, const uint8_t *from, uint32_t n) {
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(ring + (uint32_t)p_slot * S::kBlockBytes), "l"(src), "r"((uint32_t)S::kBlockBytes), "r"(bar) : "memory");
+                             ::"r"(to), "l"(from), "r"(n), "r"(bar) : "memory");
+            };
+            if (a.withhold && blockIdx.x == 0 && warp == 0) {   // (test switch: these copies are never requested)
+            } else if (bytes == 0) {
+                mbar_arrive(bar);
+            } else {
+                mbar_arrive_expect_tx(bar, bytes);
+                if (!split) {
+                    copy(dst, src + (int64_t)i0 * a.cache.page_stride, bytes);
+                } else {
+                    if (n0 > 0) copy(dst, src + (int64_t)i0 * a.cache.page_stride, S::kBlockBytes);
+                    if (n1 > 0) copy(dst + S::kBlockBytes, src + (int64_t)i1 * a.cache.page_stride, S::kBlockBytes);
+                }
             }
         }
         if (++p_slot == ST) p_slot = 0;
         p_t += kWarps;
-        settle();
+        ++p_k;
+        settle(p_t >= p_end);
     };
-    settle();
+    p_k = 64;   // (nothing settled yet)
+    settle(false);
     for (int i = 0; i < ST; ++i) request();
 
     int slot = 0;
     uint32_t phases = 0;
     bool dead = false;
-    while (u < u_end) {
-        const int t_end = min(cur.blocks(), t_at + u_end - u);
-        const int row0 = cur.chunk * ROWS, nrows = max(0, min(ROWS, cur.rows * a.group - row0));
-        const bool whole = t_at == 0 && t_end == cur.blocks();
+    while (start < u_end) {
+        const bool reads = cur.reads();
+        const int t0 = reads ? first_pair(start) : 0, t1 = reads ? last_pair(cur, start) : 1;
+        if (t1 > t0) {
+            const int row0 = cur.chunk * ROWS, nrows = max(0, min(ROWS, cur.rows * a.group - row0));
+            const bool whole = !reads || (t0 == 0 && t1 == cur.nb);
 
-        // ---- Q of this row tile: row i * group + h of the kv head's rows, scaled to fp16
-        if ((a.kd < D || a.idx_feat != nullptr) && nrows > 0) {
-            keep_features<D>(a, cur.b, cur.hk, cur.rows, row0, nrows, t_at == 0, kept);
-            __syncthreads();
-        }
-        for (int r = warp; r < ROWS; r += kWarps) {
-            const int i = (row0 + r) / a.group, h = (row0 + r) - i * a.group;
-            float x[W32], top = 0.f;
+            // ---- Q of this row tile: row i * group + h of the kv head's rows, scaled to fp16
 #pragma unroll
-            for (int v = 0; v < W32; ++v) {
-                x[v] = 0.f;
+            for (int r0 = 0; r0 < ROWS; r0 += kWarps) {
+                const int r = r0 + warp, i = (row0 + r) / a.group, h = (row0 + r) - i * a.group;
+                const int64_t head = (int64_t)cur.hk * a.group + h;
+                float x[W32], top = 0.f;
+#pragma unroll
+                for (int v = 0; v < W32; ++v) x[v] = 0.f;
                 if (r < nrows) {
-                    const bool in = a.kd == D || (kept[(r % a.group) * W32 + v] >> lane & 1u);
-                    if (in) x[v] = __bfloat162float(a.q[cur.b * a.q_sb + ((int64_t)cur.hk * a.group + h) * a.q_sh + (int64_t)i * a.q_sr + v * 32 + lane]);
+                    const __nv_bfloat16 *qp = a.q + cur.b * a.q_sb + head * a.q_sh + (int64_t)i * a.q_sr + lane;
+                    const uint32_t *kp = a.kept + ((int64_t)cur.b * a.Hkv * a.group + head) * W32;
+#pragma unroll
+                    for (int v = 0; v < W32; ++v) x[v] = __bfloat162float(qp[v * 32]);
+                    if (a.kept != nullptr)
+#pragma unroll
+                        for (int v = 0; v < W32; ++v) x[v] = kp[v] >> lane & 1u ? x[v] : 0.f;
                 }
-                top = fmaxf(top, fabsf(x[v]));
-            }
-            top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-            // 2^e at top; a row of zeros, or one too small or large to scale, is taken as it is
-            const int e = (int)(__float_as_uint(top) >> 23) - 127;
-            const int shift = e < -100 || e > 100 ? 0 : 14 - e;
-            const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
 #pragma unroll
-            for (int v = 0; v < W32; ++v)   // odd columns meet codes that lie four bits up
-                qs[r * S::kPitchQ + v * 32 + lane] = __float2half_rn(x[v] * up * (lane & 1 ? 0.0625f : 1.f));
+                for (int v = 0; v < W32; ++v) top = fmaxf(top, fabsf(x[v]));
+                top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+                // 2^e at top; a row of zeros, or one too small or large to scale, is taken as it is
+                const int e = (int)(__float_as_uint(top) >> 23) - 127;
+                const int shift = e < -100 || e > 100 ? 0 : 14 - e;
+                const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+                // Column 8 t + c of 32: lane 4 (r % 8) + t, words (c = 0, 4) (1, 5) (2, 6) (3, 7).  Odd columns meet codes four bits up.
+                const int c = lane & 7, at = ((r & 7) * 4 + (lane >> 3)) * 8 + (c & 3) * 2 + (c >> 2);
 #pragma unroll
-            for (int j = 0; j < NG; ++j) {
-                float sum = x[2 * j] + x[2 * j + 1];
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                if (lane == 0) row_sum[r * NG + j] = sum * a.scale_log2;
-            }
-            if (lane == 0) {
-                row_scale[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - shift + 24) << 23);
-                row_vis[r] = r < nrows ? (a.causal ? max(0, min(cur.len, cur.len - cur.rows + i + 1)) : cur.len) : 0;
-            }
-        }
-        __syncthreads();
-        uint32_t qf[NT][D / 16][2];
-        float cq[NT][2], qsum[NT][2][NG], m[NT][2], l[NT][2], low[NT][2][NG], o[NT][D / 16][4];
-        int vis[NT][2], vis_least = cur.len;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                // step ks: columns 32 (ks / 2) + 8 t4 + {0, 4} and {1, 5}, or {2, 6} and {3, 7}
-                const __half *p = qs + (nt * 8 + g) * S::kPitchQ + (ks >> 1) * 32 + t4 * 8 + (ks & 1) * 2;
-                qf[nt][ks][0] = (uint32_t)__half_as_ushort(p[0]) | (uint32_t)__half_as_ushort(p[4]) << 16;
-                qf[nt][ks][1] = (uint32_t)__half_as_ushort(p[1]) | (uint32_t)__half_as_ushort(p[5]) << 16;
-            }
-#pragma unroll
-            for (int mt = 0; mt < D / 16; ++mt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[nt][mt][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = nt * 8 + 2 * t4 + e;
-                cq[nt][e] = row_scale[r];
-                vis[nt][e] = row_vis[r];
-                m[nt][e] = -INFINITY;
-                l[nt][e] = 0.f;
+                for (int v = 0; v < W32; ++v) qs[((r >> 3) * W32 + v) * 256 + at] = __float2half_rn(x[v] * up * (lane & 1 ? 0.0625f : 1.f));
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
-                    qsum[nt][e][j] = row_sum[r * NG + j];
-                    low[nt][e][j] = 0.f;
+                    float sum = x[2 * j] + x[2 * j + 1];
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    if (lane == 0) row_sum[r * NG + j] = sum * a.scale_log2;
+                }
+                if (lane == 0) {
+                    row_scale[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - shift + 24) << 23);
+                    row_vis[r] = r < nrows ? (a.causal ? max(0, min(cur.len, cur.len - cur.rows + i + 1)) : cur.len) : 0;
                 }
             }
-        }
-        for (int r = 0; r < nrows; ++r) vis_least = min(vis_least, row_vis[r]);
-
-        if (cur.reads()) {
-            for (int t = t_at + warp; t < t_end; t += kWarps) {
-                dead = dead || !mbar_wait(bars + 8 * slot, phases >> slot & 1u, &abort_flag, a.status, a.wait_ns);
-                if (dead) continue;   // (gave up: no more copies, but every meeting of the block and of the CTAs is kept)
-                phases ^= 1u << slot;
-                const uint8_t *blk = smem + (warp * ST + slot) * S::kBlockBytes;
-                const int held = tokens[slot];
-                // -- S^T = K Q^T
-                float acc[NT][NG][4];
+            __syncthreads();
+            float cq[NT][2], qsum[NT][2][NG], nm[NT][2], l[NT][2], low[NT][2][NG], o[NT][D / 16][4];   // nm: minus the reference
+            int vis[NT][2], vis_least = cur.len;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                    for (int j = 0; j < NG; ++j)
+                for (int mt = 0; mt < D / 16; ++mt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[nt][j][e] = 0.f;
-                uint32_t k0[W32], k1[W32];
-                {
-                    const uint32_t *p0 = reinterpret_cast<const uint32_t *>(blk) + g * (D / 8) + t4 * W32, *p1 = p0 + D;
-                    if constexpr (W32 == 2) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(p0), y = *reinterpret_cast<const uint2 *>(p1);
-                        k0[0] = x.x; k0[1] = x.y; k1[0] = y.x; k1[1] = y.y;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < W32 / 4; ++i) {
-                            const uint4 x = reinterpret_cast<const uint4 *>(p0)[i], y = reinterpret_cast<const uint4 *>(p1)[i];
-                            k0[4 * i] = x.x; k0[4 * i + 1] = x.y; k0[4 * i + 2] = x.z; k0[4 * i + 3] = x.w;
-                            k1[4 * i] = y.x; k1[4 * i + 1] = y.y; k1[4 * i + 2] = y.z; k1[4 * i + 3] = y.w;
-                        }
-                    }
-                }
-#pragma unroll
-                for (int w = 0; w < W32; ++w) {
-                    const uint32_t x = k0[w], y = k1[w], xs = x >> 8, ys = y >> 8;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma_f16(acc[nt][w / 2], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][2 * w][0], qf[nt][2 * w][1]);
-                        mma_f16(acc[nt][w / 2], xs & 0x000f000fu, ys & 0x000f000fu, xs & 0x00f000f0u, ys & 0x00f000f0u, qf[nt][2 * w + 1][0], qf[nt][2 * w + 1][1]);
-                    }
-                }
-                // -- steps and least values of keys and values g and g + 8
-                float ks[2][NG], km[2][NG], vs[2][NG], vm[2][NG], ls[2];
-                const uint32_t *pairs = reinterpret_cast<const uint32_t *>(blk) + 4 * D;
-                const bool edge = held < kv4::kBlock || (t + 1) * kv4::kBlock > vis_least;
+                    for (int e = 0; e < 4; ++e) o[nt][mt][e] = 0.f;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float most = 0.f;
+                    const int r = nt * 8 + 2 * t4 + e;
+                    cq[nt][e] = row_scale[r];
+                    vis[nt][e] = row_vis[r];
+                    nm[nt][e] = kNone;
+                    l[nt][e] = 0.f;
 #pragma unroll
                     for (int j = 0; j < NG; ++j) {
-                        const uint32_t x = pairs[(g + 8 * e) * NG + j];
-                        uint32_t y = pairs[D / 4 + (g + 8 * e) * NG + j];
-                        if (edge && g + 8 * e >= held) y = 0u;   // what lies behind the last token may be anything
-                        ks[e][j] = bf16_bits(x & 0xffffu);
-                        km[e][j] = __uint_as_float(x & 0xffff0000u);
-                        vs[e][j] = bf16_bits(y & 0xffffu);
-                        vm[e][j] = __uint_as_float(y & 0xffff0000u);
-                        most = fmaxf(most, vs[e][j]);
+                        qsum[nt][e][j] = row_sum[r * NG + j];
+                        low[nt][e][j] = 0.f;
                     }
-                    ls[e] = fmaxf(lg2(most), kLeastStep);
                 }
-                float x[NT][4];
-                bool grow = false;
+            }
+            for (int r = 0; r < nrows; ++r) vis_least = min(vis_least, row_vis[r]);
+
+            // One pair of blocks.  EDGE: some of its tokens are none, or not seen by every row.
+            auto pair = [&](const uint8_t *blk, int t, int held, auto edge_tag) {
+                constexpr bool EDGE = decltype(edge_tag)::value;
+                // -- S^T = K Q^T by groups of 64 columns, with the keys' steps and least values
+                float x[2][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int j = 0; j < NG; ++j) {
+                    float acc[2][NT][4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float lin = ks[e >> 1][0] * acc[nt][0][e], off = km[e >> 1][0] * qsum[nt][e & 1][0];
+                    for (int f = 0; f < 2; ++f)
 #pragma unroll
-                        for (int j = 1; j < NG; ++j) {
-                            lin = fmaf(ks[e >> 1][j], acc[nt][j][e], lin);
-                            off = fmaf(km[e >> 1][j], qsum[nt][e & 1][j], off);
-                        }
-                        x[nt][e] = fmaf(cq[nt][e & 1], lin, off);
-                        if (edge && (g + (e >> 1) * 8 >= held || t * kv4::kBlock + g + (e >> 1) * 8 >= vis[nt][e & 1])) x[nt][e] = -INFINITY;
-                        grow |= x[nt][e] + ls[e >> 1] > m[nt][e & 1] + kGrow;
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[f][nt][e] = 0.f;
+                    uint2 k0[2], k1[2];   // words 2 j, 2 j + 1 of keys g and g + 8 of either block
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        const uint32_t *p = reinterpret_cast<const uint32_t *>(blk + f * S::kBlockBytes) + g * (D / 8) + t4 * W32 + 2 * j;
+                        k0[f] = *reinterpret_cast<const uint2 *>(p);
+                        k1[f] = *reinterpret_cast<const uint2 *>(p + D);
                     }
-                if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        uint4 qf[NT];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) qf[nt] = reinterpret_cast<const uint4 *>(qs)[(nt * W32 + 2 * j + w) * 32 + lane];
+#pragma unroll
+                        for (int f = 0; f < 2; ++f) {
+                            const uint32_t u = w ? k0[f].y : k0[f].x, v = w ? k1[f].y : k1[f].x, us = u >> 8, vs = v >> 8;
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_f16(acc[f][nt], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u, v & 0x00f000f0u, qf[nt].x, qf[nt].y);
+                                mma_f16(acc[f][nt], us & 0x000f000fu, vs & 0x000f000fu, us & 0x00f000f0u, vs & 0x00f000f0u, qf[nt].z, qf[nt].w);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int f = 0; f < 2; ++f)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t z = reinterpret_cast<const uint32_t *>(blk + f * S::kBlockBytes)[4 * D + (g + 8 * e) * NG + j];
+                            const float ks = bf16_bits(z), km = __uint_as_float(z & 0xffff0000u);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int c = 0; c < 2; ++c) {
+                                    const float y = ks * cq[nt][c], off = km * qsum[nt][c][j];
+                                    float &to = x[f][nt][2 * e + c];
+                                    to = fmaf(y, acc[f][nt][2 * e + c], j == 0 ? off : to + off);
+                                }
+                        }
+                }
+                // -- steps and least values of the values
+                float vs[2][2][NG], vm[2][2][NG], most[2][2];
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int n = f ? held >> 8 : held & 255;
+                        most[f][e] = kLeastStep;
+#pragma unroll
+                        for (int j = 0; j < NG; ++j) {
+                            uint32_t z = reinterpret_cast<const uint32_t *>(blk + f * S::kBlockBytes)[4 * D + D / 4 + (g + 8 * e) * NG + j];
+                            if (EDGE && g + 8 * e >= n) z = 0u;   // what lies behind the last token may be anything
+                            vs[f][e][j] = bf16_bits(z);
+                            vm[f][e][j] = __uint_as_float(z & 0xffff0000u);
+                            most[f][e] = fmaxf(most[f][e], vs[f][e][j]);
+                        }
+                        if (EDGE) {
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int c = 0; c < 2; ++c)
+                                    if (g + 8 * e >= n || t * kPair + f * kv4::kBlock + g + 8 * e >= vis[nt][c]) x[f][nt][2 * e + c] = -INFINITY;
+                        }
+                    }
+                // -- weights
+                float p[2][NT][4];
+                auto weights = [&]() {
+                    float top = 0.f;
+#pragma unroll
+                    for (int f = 0; f < 2; ++f)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                p[f][nt][e] = ex2(x[f][nt][e] + nm[nt][e & 1]);
+                                top = fmaxf(top, p[f][nt][e] * most[f][e >> 1]);
+                            }
+                    return top;
+                };
+                if (__any_sync(0xffffffffu, weights() > kTopWeight)) {   // the rows' references move, and the sums taken against the old ones are scaled
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float mx = fmaxf(x[nt][e] + ls[0], x[nt][e + 2] + ls[1]);
+                        for (int c = 0; c < 2; ++c) {
+                            float mx = -INFINITY;
+#pragma unroll
+                            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) mx = fmaxf(mx, x[f][nt][2 * e + c] + lg2(most[f][e]));
 #pragma unroll
                             for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                            mx = fmaxf(mx - kTop, m[nt][e]);
-                            const float alpha = m[nt][e] > -INFINITY ? ex2(m[nt][e] - mx) : 1.f;
-                            m[nt][e] = mx;
-                            l[nt][e] *= alpha;
+                            const float to = fminf(kTop - mx, nm[nt][c]), alpha = ex2(to - nm[nt][c]);
+                            nm[nt][c] = to;
+                            l[nt][c] *= alpha;
 #pragma unroll
-                            for (int j = 0; j < NG; ++j) low[nt][e][j] *= alpha;
+                            for (int j = 0; j < NG; ++j) low[nt][c][j] *= alpha;
 #pragma unroll
                             for (int mt = 0; mt < D / 16; ++mt) {
-                                o[nt][mt][e] *= alpha;
-                                o[nt][mt][e + 2] *= alpha;
+                                o[nt][mt][c] *= alpha;
+                                o[nt][mt][c + 2] *= alpha;
                             }
                         }
+                    weights();
                 }
-                uint32_t pb[NT][NG][2];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float p[4];
+                for (int f = 0; f < 2; ++f) {
+                    uint32_t pb[NT][NG][2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[e] = ex2(x[nt][e] + (m[nt][e & 1] > -INFINITY ? -m[nt][e & 1] : 0.f));
-                    l[nt][0] += p[0] + p[2];
-                    l[nt][1] += p[1] + p[3];
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float *pp = p[f][nt];
+                        l[nt][0] += pp[0] + pp[2];
+                        l[nt][1] += pp[1] + pp[3];
 #pragma unroll
-                    for (int j = 0; j < NG; ++j) {
-                        low[nt][0][j] = fmaf(p[0], vm[0][j], fmaf(p[2], vm[1][j], low[nt][0][j]));
-                        low[nt][1][j] = fmaf(p[1], vm[0][j], fmaf(p[3], vm[1][j], low[nt][1][j]));
-                        pb[nt][j][0] = transpose8x8(pack_f16(p[0] * vs[0][j], p[1] * vs[0][j]));   // (key g, rows 2 t4) -> (row g, keys 2 t4)
-                        pb[nt][j][1] = transpose8x8(pack_f16(p[2] * vs[1][j], p[3] * vs[1][j]));
-                    }
-                }
-                // -- O^T += V^T P^T: lane (g, t4) has the columns 64 j + 8 g .. of tokens 2 t4, 2 t4 + 1 and those 8 on
-                const uint32_t *vp = reinterpret_cast<const uint32_t *>(blk) + 2 * D;
-                auto columns = [&](int j, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const uint32_t sel = half ? 0x7632u : 0x5410u;
-                        uint32_t x = __byte_perm(w0, w1, sel), y = __byte_perm(w2, w3, sel);
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-                                mma_f16(o[nt][j * 4 + half * 2 + q], x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u, pb[nt][j][0], pb[nt][j][1]);
-                            x >>= 8;
-                            y >>= 8;
+                        for (int j = 0; j < NG; ++j) {
+                            low[nt][0][j] = fmaf(pp[0], vm[f][0][j], fmaf(pp[2], vm[f][1][j], low[nt][0][j]));
+                            low[nt][1][j] = fmaf(pp[1], vm[f][0][j], fmaf(pp[3], vm[f][1][j], low[nt][1][j]));
+                            pb[nt][j][0] = transpose8x8(pack_f16(pp[0] * vs[f][0][j], pp[1] * vs[f][0][j]));   // (key g, rows 2 t4) -> (row g, keys 2 t4)
+                            pb[nt][j][1] = transpose8x8(pack_f16(pp[2] * vs[f][1][j], pp[3] * vs[f][1][j]));
                         }
                     }
-                };
-                if constexpr (D == 64) {
-                    const uint2 x = reinterpret_cast<const uint2 *>(vp)[lane], y = reinterpret_cast<const uint2 *>(vp)[32 + lane];
-                    columns(0, x.x, x.y, y.x, y.y);
-                } else {
+                    // -- O^T += V^T P^T: lane (g, t4) has the columns 64 j + 8 g .. of tokens 2 t4, 2 t4 + 1 and those 8 on
+                    const uint8_t *vp = blk + f * S::kBlockBytes + 8 * D;
+                    auto columns = [&](int j, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
 #pragma unroll
-                    for (int i = 0; i < D / 128; ++i) {
-                        const uint4 x = reinterpret_cast<const uint4 *>(vp)[(2 * i) * 32 + lane], y = reinterpret_cast<const uint4 *>(vp)[(2 * i + 1) * 32 + lane];
-                        columns(2 * i, x.x, x.z, y.x, y.z);
-                        columns(2 * i + 1, x.y, x.w, y.y, y.w);
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t sel = half ? 0x7632u : 0x5410u;
+                            uint32_t u = __byte_perm(w0, w1, sel), v = __byte_perm(w2, w3, sel);
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+                                    mma_f16(o[nt][j * 4 + half * 2 + q], u & 0x000f000fu, u & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u, pb[nt][j][0], pb[nt][j][1]);
+                                u >>= 8;
+                                v >>= 8;
+                            }
+                        }
+                    };
+                    if constexpr (D == 64) {
+                        const uint2 u = reinterpret_cast<const uint2 *>(vp)[lane], v = reinterpret_cast<const uint2 *>(vp)[32 + lane];
+                        columns(0, u.x, u.y, v.x, v.y);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < D / 128; ++i) {
+                            const uint4 u = reinterpret_cast<const uint4 *>(vp)[(2 * i) * 32 + lane], v = reinterpret_cast<const uint4 *>(vp)[(2 * i + 1) * 32 + lane];
+                            columns(2 * i, u.x, u.z, v.x, v.z);
+                            columns(2 * i + 1, u.y, u.w, v.y, v.w);
+                        }
                     }
                 }
-                __syncwarp();   // every lane is done with this entry
-                if (++slot == ST) slot = 0;
-                request();
+            };
+            if (reads) {
+                for (int t = t0 + warp; t < t1; t += kWarps) {
+                    dead = dead || !mbar_wait(bars + 8 * slot, phases >> slot & 1u, &abort_flag, a.status, a.wait_ns);
+                    if (dead) continue;   // (gave up: no more copies, but every meeting of the block and of the CTAs is kept)
+                    phases ^= 1u << slot;
+                    const uint8_t *blk = smem + (warp * ST + slot) * S::kPairBytes;
+                    const int held = tokens[slot];
+                    if (held == (kv4::kBlock | kv4::kBlock << 8) && (t + 1) * kPair <= vis_least) pair(blk, t, held, std::false_type{});
+                    else pair(blk, t, held, std::true_type{});
+                    __syncwarp();   // every lane is done with this entry
+                    if (++slot == ST) slot = 0;
+                    request();
+                }
             }
-        }
 
-        // ---- the warps meet
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int d = 4; d < 32; d <<= 1) {
-                    l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], d);
-#pragma unroll
-                    for (int j = 0; j < NG; ++j) low[nt][e][j] += __shfl_xor_sync(0xffffffffu, low[nt][e][j], d);
-                }
-                if (g == 0) {
-                    ml[(warp * ROWS + nt * 8 + 2 * t4 + e) * 2] = m[nt][e];
-                    ml[(warp * ROWS + nt * 8 + 2 * t4 + e) * 2 + 1] = l[nt][e];
-                }
-            }
-        __syncthreads();
-        if (tid < ROWS) {
-            float mx = -INFINITY, sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * ROWS + tid) * 2]);
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float mw = ml[(w * ROWS + tid) * 2], lw = ml[(w * ROWS + tid) * 2 + 1];
-                const float f = mw > -INFINITY ? ex2(mw - mx) : 0.f;
-                // (a NaN among a row's logits is in its sum, though the reference may have passed it by)
-                sum += mw > -INFINITY ? f * lw : lw;
-                ml[(w * ROWS + tid) * 2] = f;
-            }
-            tot[tid * 2] = mx;
-            tot[tid * 2 + 1] = tid < nrows ? sum : 0.f;   // (rows that are none have met keys all the same)
-        }
-        float *part = nullptr;
-        if (!whole) part = a.part + (int64_t)(2 * blockIdx.x + (t_at == 0 ? 1 : 0)) * ROWS * (D + 2);
-#pragma unroll
-        for (int j = 0; j < NG; ++j) {
-            if (j > 0) __syncthreads();
+            // ---- the warps meet
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float *dst = merge + (warp * ROWS + nt * 8 + 2 * t4 + e) * S::kPitchM + 8 * g;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)   // columns 8 g + 2 q and the next, whose codes lay four bits up
-                        *reinterpret_cast<float2 *>(dst + 2 * q) = make_float2(fmaf(o[nt][j * 4 + q][e], 16777216.f, low[nt][e][j]),
-                                                                               fmaf(o[nt][j * 4 + q][e + 2], 1048576.f, low[nt][e][j]));
+                    for (int d = 4; d < 32; d <<= 1) {
+                        l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], d);
+#pragma unroll
+                        for (int j = 0; j < NG; ++j) low[nt][e][j] += __shfl_xor_sync(0xffffffffu, low[nt][e][j], d);
+                    }
+                    if (g == 0) {
+                        ml[(warp * ROWS + nt * 8 + 2 * t4 + e) * 2] = -nm[nt][e];
+                        ml[(warp * ROWS + nt * 8 + 2 * t4 + e) * 2 + 1] = l[nt][e];
+                    }
                 }
             __syncthreads();
-            for (int i = tid; i < ROWS * 64; i += kWarps * 32) {
-                const int r = i >> 6, c = i & 63;
-                float sum = 0.f;
+            if (tid < ROWS) {
+                float mx = -kNone, sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[(w * ROWS + tid) * 2]);
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) {
-                    const float f = ml[(w * ROWS + r) * 2];
-                    sum += f != 0.f ? f * merge[(w * ROWS + r) * S::kPitchM + c] : 0.f;
+                    const float f = ex2(ml[(w * ROWS + tid) * 2] - mx);   // (a NaN among a row's logits is in its sum)
+                    sum = fmaf(f, ml[(w * ROWS + tid) * 2 + 1], sum);
+                    ml[(w * ROWS + tid) * 2] = f;
                 }
-                const float lsum = tot[r * 2 + 1];
-                if (whole) {
-                    const int row = row0 + r, qi = row / a.group;
-                    if (qi < a.L)
-                        a.o[cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr + j * 64 + c] =
-                            __float2bfloat16_rn(lsum == 0.f ? 0.f : sum * (1.f / lsum));   // (0: the row sees no key; a NaN stays one)
-                } else {
-                    part[r * (D + 2) + j * 64 + c] = sum;
-                    if (j == 0 && c < 2) part[r * (D + 2) + D + c] = tot[r * 2 + c];
-                }
+                tot[tid * 2] = mx;
+                tot[tid * 2 + 1] = tid < nrows ? sum : 0.f;   // (rows that are none have met keys all the same)
             }
-        }
-        __syncthreads();
-
-        // ---- a job that other CTAs work on too: whichever comes last adds the parts up
-        if (!whole) {
-            const int job0 = u - t_at, job1 = job0 + cur.blocks() - 1;   // its first and last place on the axis
-            const int c0 = (int)((((int64_t)job0 + 1) * ctas - 1) / total), c1 = (int)((((int64_t)job1 + 1) * ctas - 1) / total);
-            const unsigned n = (unsigned)(c1 - c0 + 1);
-            if (tid == 0) {
-                __threadfence();
-                s_last = atomicInc(a.counters + c0, n - 1u) == n - 1u;
-                __threadfence();
+            float *part = whole ? nullptr : a.part + (int64_t)(2 * blockIdx.x + (t0 == 0 ? 1 : 0)) * ROWS * (D + 2);
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                if (j > 0) __syncthreads();
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float *dst = merge + (warp * ROWS + nt * 8 + 2 * t4 + e) * S::kPitchM + 8 * g;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)   // columns 8 g + 2 q and the next, whose codes lay four bits up
+                            *reinterpret_cast<float2 *>(dst + 2 * q) = make_float2(fmaf(o[nt][j * 4 + q][e], 16777216.f, low[nt][e][j]),
+                                                                                   fmaf(o[nt][j * 4 + q][e + 2], 1048576.f, low[nt][e][j]));
+                    }
+                __syncthreads();
+#pragma unroll 4
+                for (int i = tid; i < ROWS * 64; i += THREADS) {
+                    const int r = i >> 6, c = i & 63;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) sum = fmaf(ml[(w * ROWS + r) * 2], merge[(w * ROWS + r) * S::kPitchM + c], sum);
+                    const float lsum = tot[r * 2 + 1];
+                    if (whole) {
+                        const int row = row0 + r, qi = row / a.group;
+                        if (qi < a.L)
+                            a.o[cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr + j * 64 + c] =
+                                __float2bfloat16_rn(lsum == 0.f ? 0.f : sum * (1.f / lsum));   // (0: the row sees no key; a NaN stays one)
+                    } else {
+                        part[r * (D + 2) + j * 64 + c] = sum;
+                        if (j == 0 && c < 2) part[r * (D + 2) + D + c] = tot[r * 2 + c];
+                    }
+                }
             }
             __syncthreads();
-            if (s_last) {
-                for (int r = warp; r < ROWS; r += kWarps) {
-                    const int row = row0 + r, qi = row / a.group;
-                    if (qi >= a.L) continue;
-                    const float *src = a.part + r * (D + 2);
-                    auto at = [&](int c) { return src + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * ROWS * (D + 2); };
-                    float mx = -INFINITY;
-                    for (int c = c0 + lane; c <= c1; c += 32) mx = fmaxf(mx, __ldcg(at(c) + D));
+
+            // ---- a job that other CTAs work on too: whichever comes last adds the parts up
+            if (!whole) {
+                const int job0 = start + kFixed, job1 = job0 + cur.nb - 1;   // its first and last pair on the axis
+                const int c0 = (int)((((int64_t)job0 + 1) * ctas - 1) / total), c1 = (int)((((int64_t)job1 + 1) * ctas - 1) / total);
+                const unsigned n = (unsigned)(c1 - c0 + 1);
+                if (tid == 0) {
+                    __threadfence();
+                    s_last = atomicInc(a.counters + c0, n - 1u) == n - 1u;
+                    __threadfence();
+                }
+                __syncthreads();
+                if (s_last) {
+                    for (int r = warp; r < ROWS; r += kWarps) {
+                        const int row = row0 + r, qi = row / a.group;
+                        if (qi >= a.L) continue;
+                        const float *src = a.part + r * (D + 2);
+                        auto at = [&](int c) { return src + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * ROWS * (D + 2); };
+                        float mx = -kNone;
+                        for (int c = c0 + lane; c <= c1; c += 32) mx = fmaxf(mx, __ldcg(at(c) + D));
 #pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                    float sum[W32], lsum = 0.f;
+                        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                        float sum[W32], lsum = 0.f;
 #pragma unroll
-                    for (int i = 0; i < W32; ++i) sum[i] = 0.f;
+                        for (int i = 0; i < W32; ++i) sum[i] = 0.f;
 #pragma unroll 4
-                    for (int c = c0; c <= c1; ++c) {
-                        const float mw = __ldcg(at(c) + D), lw = __ldcg(at(c) + D + 1), f = mw > -INFINITY ? ex2(mw - mx) : 0.f;
-                        lsum += mw > -INFINITY ? f * lw : lw;
+                        for (int c = c0; c <= c1; ++c) {
+                            const float f = ex2(__ldcg(at(c) + D) - mx);
+                            lsum = fmaf(f, __ldcg(at(c) + D + 1), lsum);
 #pragma unroll
-                        for (int i = 0; i < W32; ++i) {
-                            const float v = __ldcg(at(c) + i * 32 + lane);
-                            sum[i] += f != 0.f ? f * v : 0.f;
+                            for (int i = 0; i < W32; ++i) sum[i] = fmaf(f, __ldcg(at(c) + i * 32 + lane), sum[i]);
                         }
-                    }
-                    const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-                    __nv_bfloat16 *o = a.o + cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr;
+                        const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+                        __nv_bfloat16 *o = a.o + cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr;
 #pragma unroll
-                    for (int i = 0; i < W32; ++i) o[i * 32 + lane] = __float2bfloat16_rn(lsum == 0.f ? 0.f : sum[i] * inv);
+                        for (int i = 0; i < W32; ++i) o[i * 32 + lane] = __float2bfloat16_rn(lsum == 0.f ? 0.f : sum[i] * inv);
+                    }
                 }
             }
         }
-        u += t_end - t_at;
-        t_at = 0;
-        if (u < u_end) cursor_next<ROWS>(a, cur);
+        start += cur.cost();
+        if (start < u_end) job_next<ROWS>(a, cur);
     }
     if (dead) drain_copies();
 }
@@ -652,14 +714,17 @@ int launch(const AttnArgs &a, cudaStream_t stream)
 
 bool kv4_attn_fits(const Kv4AttnProblem &p, const kv4::View &cache)
 {
-    // the axis of all blocks is counted in 32 bits
+    // the axis of all pairs is counted in 32 bits
     const double chunks = (double)ceil_div(p.Hq / p.Hkv * p.L, 8 * row_tiles(p));
-    return (double)p.B * p.Hkv * chunks * ((double)(cache.max_pages << cache.page_shift) + 1.0) < 2147483647.0 && p.Hq / p.Hkv * p.L < INT32_MAX / 2;
+    return (double)p.B * p.Hkv * chunks * (0.5 * (double)(cache.max_pages << cache.page_shift) + 1.0 + kFixed) < 2147483647.0 && p.Hq / p.Hkv * p.L < INT32_MAX / 2 &&
+           p.B * p.Hq < INT32_MAX;
 }
+
+static size_t parts_bytes(const Kv4AttnProblem &p) { return align_up((size_t)sm_count() * 4 * 2 * 8 * row_tiles(p) * (p.D + 2) * 4, 256); }
 
 size_t kv4_attn_workspace_bytes(const Kv4AttnProblem &p)
 {
-    return (size_t)sm_count() * 2 * 2 * 8 * row_tiles(p) * (p.D + 2) * 4;
+    return parts_bytes(p) + (size_t)(p.B * p.Hq * p.D / 8);
 }
 
 int launch_kv4_attn(const Kv4AttnProblem &p, const kv4::View &cache, float *scratch, unsigned *counters, int *status, cudaStream_t stream)
@@ -674,12 +739,19 @@ int launch_kv4_attn(const Kv4AttnProblem &p, const kv4::View &cache, float *scra
     a.B = (int)p.B; a.Hkv = (int)p.Hkv; a.group = (int)(p.Hq / p.Hkv); a.L = (int)p.L; a.kd = (int)p.kd; a.causal = p.causal;
     a.chunks = (int)ceil_div((int64_t)a.group * a.L, 8 * nt);
     a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p.D));
-    a.idx_feat = p.idx_feat;
     a.part = scratch;
     a.counters = counters;
     a.status = status;
     a.wait_ns = wait_limit_ns();
     a.withhold = debug_withhold() == WITHHOLD_KV4;
+    if (p.kd < p.D || p.idx_feat != nullptr) {
+        uint32_t *kept = reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(scratch) + parts_bytes(p));
+        auto kern = p.D == 64 ? kv4_features_kernel<2> : (p.D == 128 ? kv4_features_kernel<4> : kv4_features_kernel<8>);
+        prof_begin("kv4_features_kernel", stream);
+        launch_kernel(kern, dim3((unsigned)ceil_div(p.B * p.Hq, 4)), dim3(128), 0, stream, 1, a, kept, p.idx_feat);
+        if (int rc = check_launch("kv4_features_kernel", stream)) return rc;
+        a.kept = kept;
+    }
     if (p.D == 64) return nt == 1 ? launch<64, 1>(a, stream) : launch<64, 2>(a, stream);
     if (p.D == 128) return nt == 1 ? launch<128, 1>(a, stream) : launch<128, 2>(a, stream);
     return nt == 1 ? launch<256, 1>(a, stream) : launch<256, 2>(a, stream);
