@@ -13,11 +13,12 @@
 //     2^-25 against a largest weight of 2^6.
 //   - S^T = K Q^T and O^T = V^T P^T, so that the 8 columns of an instruction are query rows that share a kv head and its 16 rows are
 //     keys (or columns of V): the group's rows fill what 128-row tcgen05 tiles would pad.
-// The pairs of 16-token blocks of all jobs (sequence, kv head, row tile) form one axis that is cut into equal shares, one a CTA, whatever
-// the lengths are: they live on the device, so nothing is planned on the host and a captured call follows them.  A job counts kFixed
-// pairs more than it has, for what a CTA spends on it outside the keys.  Within a CTA every warp takes every fourth pair through a
-// ring of its own, filled by bulk copies of whole blocks, which runs on across jobs.  A job that ends in another CTA leaves its sums in
-// the workspace; the last CTA of a job to arrive adds them up, in order.
+// Lengths live on the device, so nothing is planned on the host and a captured call follows them: every CTA works its share out.
+// Work is counted in pairs of 16-token blocks; a job (sequence, kv head, row tile) counts kFixed pairs more than it has, for what a
+// CTA spends on it outside the keys.  A job of at least a CTA's equal share S is cut into floor(its cost / S) equal pieces, a CTA
+// each; the others form one axis that the remaining CTAs cut evenly.  Within a CTA every warp takes every fourth pair through a ring
+// of its own, filled by bulk copies of whole blocks, which runs on across jobs.  A job that is not one CTA's alone leaves its sums in the
+// workspace; the last CTA of it to arrive adds them up, in order.
 #include <math.h>
 
 #include <cuda_fp16.h>
@@ -32,7 +33,7 @@ namespace rmm {
 namespace {
 
 constexpr int kWarps = 4, kPair = 2 * kv4::kBlock;   // warps of a CTA; tokens of a warp's turn
-constexpr int kFixed = 12, kLeast = kFixed + 16;     // pairs that a job's fixed part counts as; the least share of a CTA
+constexpr int kFixed = 12, kLeast = kFixed + 8;      // pairs that a job's fixed part counts as; the least share of a CTA
 constexpr float kTopWeight = 16384.f, kTop = 6.f, kLeastStep = 8.2718061e-25f;   // 2^14, log2 of 2^6, 2^-80: see above; smaller steps weigh as that
 constexpr float kNone = 1e30f;                       // minus the reference of a row that has seen no key
 
@@ -56,7 +57,7 @@ template <int D, int NT>
 struct Shape {
     static constexpr int kRows = 8 * NT, kBlockBytes = 18 * D, kPairBytes = 2 * kBlockBytes, kGroups = D / 64;
     static constexpr int kCtas = D * NT <= 128 ? 4 : 2;                        // an SM
-    static constexpr int kStages = D == 64 ? 4 : (D == 128 && NT == 2 ? 4 : 2);
+    static constexpr int kStages = D == 64 ? (NT == 1 ? 4 : 3) : (D == 128 && NT == 2 ? 4 : 2);
     static constexpr int kPitchM = 66;
     static constexpr int kOffQ = kWarps * kStages * kPairBytes;                // fp16 fragments [row tile of 8][D / 32][lane][4 words]
     static constexpr int kOffMerge = kOffQ + kRows * D * 2;                    // fp32 [warp][row][pitch]
@@ -65,13 +66,27 @@ struct Shape {
     static constexpr int kOffTot = kOffRow + kRows * (2 + kGroups) * 4;        // [row]: reference, sum of the CTA
     static constexpr int kOffBar = (kOffTot + kRows * 8 + 15) / 16 * 16;       // barriers, then the tokens of each ring entry
     static constexpr int kSmem = kOffBar + kWarps * kStages * 12;
-    static_assert(kSmem <= 227 * 1024 / kCtas - 1280, "shared memory");
+    static_assert((kSmem + 1280) * kCtas <= 227 * 1024, "shared memory");   // (1 KB a CTA is the system's)
 };
+// (not volatile: the compiler may move products apart whose sums wait for one another)
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)   // the first of a chain
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// (key g, rows 2 t) -> (row g, keys 2 t)
+__device__ __forceinline__ uint32_t turned(uint32_t x)
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
@@ -86,41 +101,41 @@ __device__ __forceinline__ float lg2(float x)
     return y;
 }
 
-// A job on the axis of all jobs' pairs.
+// A job, and what it counts on the axis of the jobs that are not cut into pieces of their own.
 struct Job {
     int b, len, rows, nb, valid;   // sequence, its tokens and rows, pairs of a reading job, row tiles that hold rows
+    int each;                      // what its reading jobs count on the axis (0: they are cut into pieces)
     int hk, chunk;
     __device__ __forceinline__ bool reads() const { return chunk < valid && len > 0; }
-    __device__ __forceinline__ int cost() const { return reads() ? nb + kFixed : 1; }
+    __device__ __forceinline__ int cost() const { return chunk < valid ? each : 1; }
 };
 
 template <int ROWS>
-__device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c)
+__device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c, int share)
 {
     kv4::sequence(a.cache, c.b, c.len, c.rows, a.status);
     c.nb = (c.len + kPair - 1) / kPair;
     c.valid = (c.rows * a.group + ROWS - 1) / ROWS;
+    c.each = c.len == 0 ? 1 : (c.nb + kFixed >= share ? 0 : c.nb + kFixed);
 }
-__device__ __forceinline__ int head_cost(const AttnArgs &a, const Job &c)
+__device__ __forceinline__ int head_cost(const AttnArgs &a, const Job &c) { return c.valid * c.each + a.chunks - c.valid; }
+__device__ __forceinline__ int pieces_of(const Job &c, int share)   // of a reading job that is cut
 {
-    return c.len > 0 ? c.valid * (c.nb + kFixed) + a.chunks - c.valid : a.chunks;
-}
-template <int ROWS>
-__device__ __forceinline__ int sequence_cost(const AttnArgs &a, int b)
-{
-    Job c;
-    c.b = b;
-    job_sequence<ROWS>(a, c);
-    return a.Hkv * head_cost(a, c);
+    return min((c.nb + kFixed) / share, max(1, c.nb / kWarps));
 }
 template <int ROWS>
-__device__ __forceinline__ void job_next(const AttnArgs &a, Job &c)
+__device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int share)   // the next one that counts
 {
-    if (++c.chunk < a.chunks) return;
-    c.chunk = 0;
-    if (++c.hk < a.Hkv) return;
-    c.hk = 0;
-    if (++c.b < a.B) job_sequence<ROWS>(a, c);
+    ++c.chunk;
+    while (true) {
+        if (c.each == 0 && c.chunk < c.valid) c.chunk = c.valid;
+        if (c.chunk < a.chunks) return;
+        c.chunk = 0;
+        if (++c.hk < a.Hkv && head_cost(a, c) > 0) continue;
+        c.hk = 0;
+        if (++c.b >= a.B) return;
+        job_sequence<ROWS>(a, c, share);
+    }
 }
 
 // Kept features of one head a warp, as bit masks; the rule of every other form: squares summed in fp64, rounded to fp32, the kd
@@ -185,7 +200,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     using S = Shape<D, NT>;
     constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32, THREADS = kWarps * 32;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int s_scan[kWarps], s_begin[2], abort_flag, s_last;
+    __shared__ int s_scan[2][kWarps], s_begin[2], s_pending[2][5], abort_flag, s_last[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * ST * S::kPairBytes, bars = smem_u32(smem) + S::kOffBar + warp * ST * 8;
     int *tokens = reinterpret_cast<int *>(smem + S::kOffBar + kWarps * ST * 8) + warp * ST;   // of the first block, + 256 x of the second
@@ -201,141 +216,213 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     __syncthreads();
     pdl_wait();
 
-    // ---- this CTA's share of the axis
-    auto scan = [&](int v, int &sum) {   // inclusive, over the block
+    // ---- this CTA's share
+    auto scan = [&](int (&v)[2], int (&sum)[2]) {   // inclusive, over the block
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, v, d);
-            if (lane >= d) v += o;
+        for (int d = 1; d < 32; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int o = __shfl_up_sync(0xffffffffu, v[i], d);
+                if (lane >= d) v[i] += o;
+            }
+        __syncthreads();
+        if (lane == 31) {
+            s_scan[0][warp] = v[0];
+            s_scan[1][warp] = v[1];
         }
         __syncthreads();
-        if (lane == 31) s_scan[warp] = v;
-        __syncthreads();
-        int before = 0;
-        sum = 0;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) before += s_scan[w];
-            sum += s_scan[w];
+        for (int i = 0; i < 2; ++i) {
+            sum[i] = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                if (w == warp) v[i] += sum[i];
+                sum[i] += s_scan[i][w];
+            }
         }
-        return v + before;
     };
-    int total = 0, mine = 0, upto = 0;
+    Job cur;
+    int total = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-        int sum;
-        mine = b0 + tid < a.B ? sequence_cost<ROWS>(a, b0 + tid) : 0;
-        upto = scan(mine, sum);
-        total += sum;
+        int v[2] = {0, 0}, sum[2];
+        cur.b = b0 + tid;
+        if (cur.b < a.B) {
+            job_sequence<ROWS>(a, cur, INT32_MAX);
+            v[0] = a.Hkv * head_cost(a, cur);
+        }
+        scan(v, sum);
+        total += sum[0];
     }
-    const int ctas = min((int)gridDim.x, (total + kLeast - 1) / kLeast);
-    if ((int)blockIdx.x >= ctas) return;
-    const int u_begin = (int)((int64_t)total * blockIdx.x / ctas), u_end = (int)((int64_t)total * (blockIdx.x + 1) / ctas);
+    const int share = max(kLeast, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+    int n_pieces = 0, axis = 0, mine[2] = {0, 0}, upto[2] = {0, 0};   // CTAs with a piece of a job; what the other jobs count
+    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+        int sum[2];
+        upto[0] = upto[1] = 0;
+        if (a.B > THREADS) cur.b = b0 + tid;
+        if (cur.b < a.B) {
+            job_sequence<ROWS>(a, cur, share);
+            upto[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, share) : 0;
+            upto[1] = a.Hkv * head_cost(a, cur);
+        }
+        mine[0] = upto[0];
+        mine[1] = upto[1];
+        scan(upto, sum);
+        n_pieces += sum[0];
+        axis += sum[1];
+    }
+    const bool piece = (int)blockIdx.x < n_pieces;
+    const int ctas = min((int)gridDim.x - n_pieces, (axis + kLeast - 1) / kLeast), cta = (int)blockIdx.x - n_pieces;   // of the axis
+    if (cta >= ctas) return;
+    int u_begin = piece ? (int)blockIdx.x : (int)((int64_t)axis * cta / ctas), u_end = piece ? 0 : (int)((int64_t)axis * (cta + 1) / ctas);
     for (int b0 = 0, base = 0; b0 < a.B; b0 += THREADS) {
-        int sum = 0;
+        int sum[2] = {0, 0};
         if (a.B > THREADS) {
-            mine = b0 + tid < a.B ? sequence_cost<ROWS>(a, b0 + tid) : 0;
-            upto = scan(mine, sum);
+            cur.b = b0 + tid;
+            upto[0] = upto[1] = 0;
+            if (cur.b < a.B) {
+                job_sequence<ROWS>(a, cur, share);
+                upto[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, share) : 0;
+                upto[1] = a.Hkv * head_cost(a, cur);
+            }
+            mine[0] = upto[0];
+            mine[1] = upto[1];
+            scan(upto, sum);
         }
-        if (u_begin >= base + upto - mine && u_begin < base + upto) {
+        const int i = piece ? 0 : 1;
+        if (u_begin >= base + upto[i] - mine[i] && u_begin < base + upto[i]) {
             s_begin[0] = b0 + tid;
-            s_begin[1] = base + upto - mine;
+            s_begin[1] = base + upto[i] - mine[i];
         }
-        base += sum;
+        base += sum[i];
     }
     __syncthreads();
 
-    Job cur;
-    int start;   // where the current job begins on the axis
+    int start, piece0 = 0, pieces = 1;   // where the current job begins on the axis; a piece's job: its first CTA, its CTAs
     cur.b = s_begin[0];
-    start = s_begin[1];
-    job_sequence<ROWS>(a, cur);
-    {
-        const int per_head = head_cost(a, cur), each = cur.len > 0 ? cur.nb + kFixed : 1;
-        int off = u_begin - start;
+    job_sequence<ROWS>(a, cur, share);
+    if (piece) {
+        pieces = pieces_of(cur, share);
+        const int off = u_begin - s_begin[1], job = off / pieces, k = off - job * pieces;
+        piece0 = (int)blockIdx.x - k;
+        cur.hk = job / cur.valid;
+        cur.chunk = job - cur.hk * cur.valid;
+        cur.each = cur.nb + kFixed;   // alone on an axis of its own
+        start = 0;
+        u_begin = kFixed + (int)((int64_t)cur.nb * k / pieces);
+        u_end = kFixed + (int)((int64_t)cur.nb * (k + 1) / pieces);
+    } else {
+        const int per_head = head_cost(a, cur);
+        int off = u_begin - s_begin[1];
         cur.hk = off / per_head;
         off -= cur.hk * per_head;
-        cur.chunk = off < cur.valid * each ? off / each : cur.valid + off - cur.valid * each;
-        start = u_begin - (off < cur.valid * each ? off - cur.chunk * each : 0);
+        const bool in = off < cur.valid * cur.each;
+        cur.chunk = in ? off / cur.each : cur.valid + off - cur.valid * cur.each;
+        start = u_begin - (in ? off - cur.chunk * cur.each : 0);
     }
     // the pairs of the job at `at` that are this CTA's
     auto first_pair = [&](int at) { return max(0, u_begin - at - kFixed); };
     auto last_pair = [&](const Job &c, int at) { return min(c.nb, u_end - at - kFixed); };
 
+    // ---- Q of a row tile: row i * group + h of the kv head's rows (asked for before the keys are, whose page numbers come first)
+    constexpr int QR = ROWS / kWarps;   // rows of a warp
+    float qx[QR][W32];
+    auto load_q = [&]() {
+        const int row0 = cur.chunk * ROWS, nrows = min(ROWS, cur.rows * a.group - row0);
+#pragma unroll
+        for (int k = 0; k < QR; ++k) {
+            const int r = k * kWarps + warp, i = (row0 + r) / a.group, h = (row0 + r) - i * a.group;
+            const int64_t head = (int64_t)cur.hk * a.group + h;
+#pragma unroll
+            for (int v = 0; v < W32; ++v) qx[k][v] = 0.f;
+            if (r < nrows) {
+                const __nv_bfloat16 *qp = a.q + cur.b * a.q_sb + head * a.q_sh + (int64_t)i * a.q_sr + lane;
+                const uint32_t *kp = a.kept + ((int64_t)cur.b * a.Hkv * a.group + head) * W32;
+#pragma unroll
+                for (int v = 0; v < W32; ++v) qx[k][v] = __bfloat162float(qp[v * 32]);
+                if (a.kept != nullptr)
+#pragma unroll
+                    for (int v = 0; v < W32; ++v) qx[k][v] = kp[v] >> lane & 1u ? qx[k][v] : 0.f;
+            }
+        }
+    };
+    load_q();
+
     // ---- the warp's loads: pairs first + warp, + 4, .. of every part, ST of them under way
     Job pc = cur;
-    int p_start = start, p_t = 0, p_end = 0, p_k = 32, p_slot = 0, page0 = 0, page1 = 0;   // lanes hold the pages of the next 32 pairs
+    int p_start = start, p_t = 0, p_end = 0, p_k = 64, p_slot = 0;
+    uint64_t from0 = 0, from1 = 0;   // lanes hold where the blocks of the next 32 pairs lie,
+    int p_tokens = 0;                // and their tokens (of the first block, + 256 x of the second; 0: a page outside the pool)
     const bool split = a.cache.page_shift == 0;   // the blocks of a pair lie in two pages
-    auto settle = [&](bool next) {   // on to the next pair that has something to load
-        if (!next && p_t < p_end && p_k < 32) return;
+    auto window = [&]() {
+        const int t = p_t + lane * kWarps, left = pc.len - t * kPair;
+        int n0 = max(0, min(left, kv4::kBlock)), n1 = max(0, min(left - kv4::kBlock, kv4::kBlock));
+        const int32_t *row = a.cache.pages + pc.b * a.cache.pages_stride;
+        const uint8_t *head = a.cache.pool + pc.hk * a.cache.head_stride;
+        const int i0 = n0 > 0 ? __ldg(row + (2 * t >> a.cache.page_shift)) : 0, i1 = split && n1 > 0 ? __ldg(row + 2 * t + 1) : i0;
+        const bool good0 = i0 >= 0 && i0 < a.cache.n_pages, good1 = i1 >= 0 && i1 < a.cache.n_pages;
+        if (t < p_end && (!good0 || !good1)) atomicExch(a.status, (int)RMM_ERR_BOUNDS);
+        if (!good0) n0 = 0;
+        if (!good1) n1 = 0;
+        from0 = reinterpret_cast<uint64_t>(head + (int64_t)i0 * a.cache.page_stride + (int64_t)(2 * t & ((1 << a.cache.page_shift) - 1)) * S::kBlockBytes);
+        from1 = reinterpret_cast<uint64_t>(head + (int64_t)i1 * a.cache.page_stride);
+        p_tokens = n0 | n1 << 8;
+        p_k = 0;
+    };
+    auto settle = [&]() {   // from the end of a part on to the next pair that has something to load
         while (true) {
-            if (next) {
+            if (p_k != 64) {
                 p_start += pc.cost();
                 if (p_start >= u_end) {
                     p_t = p_end = 0;
                     return;
                 }
-                job_next<ROWS>(a, pc);
+                job_next<ROWS>(a, pc, share);
             }
-            if (next || p_k == 64) {
-                p_end = pc.reads() ? last_pair(pc, p_start) : 0;
-                p_t = first_pair(p_start) + warp;
-                p_k = 32;
-            }
+            p_end = pc.reads() ? last_pair(pc, p_start) : 0;
+            p_t = first_pair(p_start) + warp;
+            p_k = 32;
             if (p_t < p_end) break;
-            next = true;
         }
-        if (p_k == 32) {
-            const int32_t *row = a.cache.pages + pc.b * a.cache.pages_stride;
-            const int t = 2 * (p_t + lane * kWarps), blocks = (pc.len + kv4::kBlock - 1) / kv4::kBlock;   // first block of the lane's pair
-            page0 = t < blocks ? __ldg(row + (t >> a.cache.page_shift)) : 0;
-            page1 = split && t + 1 < blocks ? __ldg(row + t + 1) : page0;
-            p_k = 0;
-        }
+        window();
     };
     auto request = [&]() {
         if (p_t >= p_end) return;
-        const int i0 = __shfl_sync(0xffffffffu, page0, p_k), i1 = __shfl_sync(0xffffffffu, page1, p_k);
+        const int n = __shfl_sync(0xffffffffu, p_tokens, p_k);
+        const uint64_t src0 = __shfl_sync(0xffffffffu, from0, p_k), src1 = split ? __shfl_sync(0xffffffffu, from1, p_k) : 0;
         if (lane == 0) {
             const uint32_t bar = bars + 8 * p_slot, dst = ring + (uint32_t)p_slot * S::kPairBytes;
-            const int left = pc.len - p_t * kPair;
-            const bool good0 = i0 >= 0 && i0 < a.cache.n_pages, good1 = i1 >= 0 && i1 < a.cache.n_pages;
-            int n0 = min(left, kv4::kBlock), n1 = max(0, min(left - kv4::kBlock, kv4::kBlock));
-            if (!good0 || (n1 > 0 && !good1)) atomicExch(a.status, (int)RMM_ERR_BOUNDS);
-            if (!good0) n0 = 0;
-            if (!good1) n1 = 0;
-            tokens[p_slot] = n0 | n1 << 8;
-            const uint32_t bytes = (n0 > 0 ? S::kBlockBytes : 0) + (n1 > 0 ? S::kBlockBytes : 0);
-            const uint8_t *src = a.cache.pool + pc.hk * a.cache.head_stride +
-                                 (int64_t)((2 * p_t) & ((1 << a.cache.page_shift) - 1)) * S::kBlockBytes;
-            auto copy = [&](uint32_t to, const uint8_t *from, uint32_t n) {
+            const uint32_t b0 = n & 255 ? S::kBlockBytes : 0, b1 = n >> 8 ? S::kBlockBytes : 0;
+            auto copy = [&](uint32_t to, uint64_t from, uint32_t bytes) {
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(to), "l"(from), "r"(n), "r"(bar) : "memory");
+                             ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
             };
+            tokens[p_slot] = n;
             if (a.withhold && blockIdx.x == 0 && warp == 0) {   // (test switch: these copies are never requested)
-            } else if (bytes == 0) {
+            } else if (n == 0) {
                 mbar_arrive(bar);
             } else {
-                mbar_arrive_expect_tx(bar, bytes);
+                mbar_arrive_expect_tx(bar, b0 + b1);
                 if (!split) {
-                    copy(dst, src + (int64_t)i0 * a.cache.page_stride, bytes);
+                    copy(dst, src0, b0 + b1);
                 } else {
-                    if (n0 > 0) copy(dst, src + (int64_t)i0 * a.cache.page_stride, S::kBlockBytes);
-                    if (n1 > 0) copy(dst + S::kBlockBytes, src + (int64_t)i1 * a.cache.page_stride, S::kBlockBytes);
+                    if (b0 > 0) copy(dst, src0, b0);
+                    if (b1 > 0) copy(dst + S::kBlockBytes, src1, b1);
                 }
             }
         }
         if (++p_slot == ST) p_slot = 0;
         p_t += kWarps;
         ++p_k;
-        settle(p_t >= p_end);
+        if (p_t >= p_end) settle();
+        else if (p_k == 32) window();
     };
-    p_k = 64;   // (nothing settled yet)
-    settle(false);
+    settle();
     for (int i = 0; i < ST; ++i) request();
 
     int slot = 0;
     uint32_t phases = 0;
-    bool dead = false;
+    bool dead = false, first = true;
+    if (tid < 2) s_pending[tid][0] = -1;
     while (start < u_end) {
         const bool reads = cur.reads();
         const int t0 = reads ? first_pair(start) : 0, t1 = reads ? last_pair(cur, start) : 1;
@@ -343,23 +430,13 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             const int row0 = cur.chunk * ROWS, nrows = max(0, min(ROWS, cur.rows * a.group - row0));
             const bool whole = !reads || (t0 == 0 && t1 == cur.nb);
 
-            // ---- Q of this row tile: row i * group + h of the kv head's rows, scaled to fp16
+            // ---- Q scaled to fp16
+            if (!first) load_q();
 #pragma unroll
-            for (int r0 = 0; r0 < ROWS; r0 += kWarps) {
-                const int r = r0 + warp, i = (row0 + r) / a.group, h = (row0 + r) - i * a.group;
-                const int64_t head = (int64_t)cur.hk * a.group + h;
-                float x[W32], top = 0.f;
-#pragma unroll
-                for (int v = 0; v < W32; ++v) x[v] = 0.f;
-                if (r < nrows) {
-                    const __nv_bfloat16 *qp = a.q + cur.b * a.q_sb + head * a.q_sh + (int64_t)i * a.q_sr + lane;
-                    const uint32_t *kp = a.kept + ((int64_t)cur.b * a.Hkv * a.group + head) * W32;
-#pragma unroll
-                    for (int v = 0; v < W32; ++v) x[v] = __bfloat162float(qp[v * 32]);
-                    if (a.kept != nullptr)
-#pragma unroll
-                        for (int v = 0; v < W32; ++v) x[v] = kp[v] >> lane & 1u ? x[v] : 0.f;
-                }
+            for (int k = 0; k < QR; ++k) {
+                const int r = k * kWarps + warp, i = (row0 + r) / a.group;
+                const float (&x)[W32] = qx[k];
+                float top = 0.f;
 #pragma unroll
                 for (int v = 0; v < W32; ++v) top = fmaxf(top, fabsf(x[v]));
                 top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
@@ -376,7 +453,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     float sum = x[2 * j] + x[2 * j + 1];
 #pragma unroll
                     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                    if (lane == 0) row_sum[r * NG + j] = sum * a.scale_log2;
+                    if (lane == 0) row_sum[r * NG + j] = sum * __uint_as_float((uint32_t)(127 + shift - 24) << 23);
                 }
                 if (lane == 0) {
                     row_scale[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - shift + 24) << 23);
@@ -411,17 +488,29 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             // One pair of blocks.  EDGE: some of its tokens are none, or not seen by every row.
             auto pair = [&](const uint8_t *blk, int t, int held, auto edge_tag) {
                 constexpr bool EDGE = decltype(edge_tag)::value;
-                // -- S^T = K Q^T by groups of 64 columns, with the keys' steps and least values
+                // -- S^T = K Q^T by groups of 64 columns, with the keys' steps and least values: logits in units of cq
                 float x[2][NT][4];
+                uint32_t kz[2][2][NG], vz[2][2][NG];   // (step, least value) of keys and values g and g + 8 of either block
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t *z = reinterpret_cast<const uint32_t *>(blk + f * S::kBlockBytes) + 4 * D + (g + 8 * e) * NG;
+                        if constexpr (NG == 1) {
+                            kz[f][e][0] = z[0];
+                            vz[f][e][0] = z[D / 4];
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < NG; j += 2) {
+                                const uint2 k = *reinterpret_cast<const uint2 *>(z + j), v = *reinterpret_cast<const uint2 *>(z + D / 4 + j);
+                                kz[f][e][j] = k.x; kz[f][e][j + 1] = k.y;
+                                vz[f][e][j] = v.x; vz[f][e][j + 1] = v.y;
+                            }
+                        }
+                    }
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
                     float acc[2][NT][4];
-#pragma unroll
-                    for (int f = 0; f < 2; ++f)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[f][nt][e] = 0.f;
                     uint2 k0[2], k1[2];   // words 2 j, 2 j + 1 of keys g and g + 8 of either block
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
@@ -439,7 +528,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                             const uint32_t u = w ? k0[f].y : k0[f].x, v = w ? k1[f].y : k1[f].x, us = u >> 8, vs = v >> 8;
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                mma_f16(acc[f][nt], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u, v & 0x00f000f0u, qf[nt].x, qf[nt].y);
+                                if (w == 0) mma_f16_zero(acc[f][nt], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u, v & 0x00f000f0u, qf[nt].x, qf[nt].y);
+                                else mma_f16(acc[f][nt], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u, v & 0x00f000f0u, qf[nt].x, qf[nt].y);
                                 mma_f16(acc[f][nt], us & 0x000f000fu, vs & 0x000f000fu, us & 0x00f000f0u, vs & 0x00f000f0u, qf[nt].z, qf[nt].w);
                             }
                         }
@@ -448,15 +538,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     for (int f = 0; f < 2; ++f)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const uint32_t z = reinterpret_cast<const uint32_t *>(blk + f * S::kBlockBytes)[4 * D + (g + 8 * e) * NG + j];
-                            const float ks = bf16_bits(z), km = __uint_as_float(z & 0xffff0000u);
+                            const float ks = bf16_bits(kz[f][e][j]), km = __uint_as_float(kz[f][e][j] & 0xffff0000u);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                                 for (int c = 0; c < 2; ++c) {
-                                    const float y = ks * cq[nt][c], off = km * qsum[nt][c][j];
                                     float &to = x[f][nt][2 * e + c];
-                                    to = fmaf(y, acc[f][nt][2 * e + c], j == 0 ? off : to + off);
+                                    const float lin = j == 0 ? ks * acc[f][nt][2 * e + c] : fmaf(ks, acc[f][nt][2 * e + c], to);
+                                    to = fmaf(km, qsum[nt][c][j], lin);
                                 }
                         }
                 }
@@ -470,11 +559,16 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                         most[f][e] = kLeastStep;
 #pragma unroll
                         for (int j = 0; j < NG; ++j) {
-                            uint32_t z = reinterpret_cast<const uint32_t *>(blk + f * S::kBlockBytes)[4 * D + D / 4 + (g + 8 * e) * NG + j];
+                            uint32_t z = vz[f][e][j];
                             if (EDGE && g + 8 * e >= n) z = 0u;   // what lies behind the last token may be anything
                             vs[f][e][j] = bf16_bits(z);
                             vm[f][e][j] = __uint_as_float(z & 0xffff0000u);
-                            most[f][e] = fmaxf(most[f][e], vs[f][e][j]);
+                        }
+                        if constexpr (NG == 1) {
+                            most[f][e] = fmaxf(kLeastStep, vs[f][e][0]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < NG; j += 2) most[f][e] = fmax3(most[f][e], vs[f][e][j], vs[f][e][j + 1]);
                         }
                         if (EDGE) {
 #pragma unroll
@@ -493,9 +587,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                p[f][nt][e] = ex2(x[f][nt][e] + nm[nt][e & 1]);
-                                top = fmaxf(top, p[f][nt][e] * most[f][e >> 1]);
+                            for (int e = 0; e < 4; e += 2) {
+                                p[f][nt][e] = ex2(fmaf(x[f][nt][e], cq[nt][0], nm[nt][0]));
+                                p[f][nt][e + 1] = ex2(fmaf(x[f][nt][e + 1], cq[nt][1], nm[nt][1]));
+                                top = fmax3(top, p[f][nt][e] * most[f][e >> 1], p[f][nt][e + 1] * most[f][e >> 1]);
                             }
                     return top;
                 };
@@ -508,7 +603,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
 #pragma unroll
                             for (int f = 0; f < 2; ++f)
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) mx = fmaxf(mx, x[f][nt][2 * e + c] + lg2(most[f][e]));
+                                for (int e = 0; e < 2; ++e) mx = fmaxf(mx, fmaf(x[f][nt][2 * e + c], cq[nt][c], lg2(most[f][e])));
 #pragma unroll
                             for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                             const float to = fminf(kTop - mx, nm[nt][c]), alpha = ex2(to - nm[nt][c]);
@@ -536,8 +631,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                         for (int j = 0; j < NG; ++j) {
                             low[nt][0][j] = fmaf(pp[0], vm[f][0][j], fmaf(pp[2], vm[f][1][j], low[nt][0][j]));
                             low[nt][1][j] = fmaf(pp[1], vm[f][0][j], fmaf(pp[3], vm[f][1][j], low[nt][1][j]));
-                            pb[nt][j][0] = transpose8x8(pack_f16(pp[0] * vs[f][0][j], pp[1] * vs[f][0][j]));   // (key g, rows 2 t4) -> (row g, keys 2 t4)
-                            pb[nt][j][1] = transpose8x8(pack_f16(pp[2] * vs[f][1][j], pp[3] * vs[f][1][j]));
+                            pb[nt][j][0] = turned(pack_f16(pp[0] * vs[f][0][j], pp[1] * vs[f][0][j]));
+                            pb[nt][j][1] = turned(pack_f16(pp[2] * vs[f][1][j], pp[3] * vs[f][1][j]));
                         }
                     }
                     // -- O^T += V^T P^T: lane (g, t4) has the columns 64 j + 8 g .. of tokens 2 t4, 2 t4 + 1 and those 8 on
@@ -572,7 +667,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             };
             if (reads) {
                 for (int t = t0 + warp; t < t1; t += kWarps) {
-                    dead = dead || !mbar_wait(bars + 8 * slot, phases >> slot & 1u, &abort_flag, a.status, a.wait_ns);
+                    if (!dead && !__all_sync(0xffffffffu, mbar_try_wait(bars + 8 * slot, phases >> slot & 1u)))
+                        dead = !mbar_wait(bars + 8 * slot, phases >> slot & 1u, &abort_flag, a.status, a.wait_ns);
                     if (dead) continue;   // (gave up: no more copies, but every meeting of the block and of the CTAs is kept)
                     phases ^= 1u << slot;
                     const uint8_t *blk = smem + (warp * ST + slot) * S::kPairBytes;
@@ -650,47 +746,67 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             }
             __syncthreads();
 
-            // ---- a job that other CTAs work on too: whichever comes last adds the parts up
-            if (!whole) {
-                const int job0 = start + kFixed, job1 = job0 + cur.nb - 1;   // its first and last pair on the axis
-                const int c0 = (int)((((int64_t)job0 + 1) * ctas - 1) / total), c1 = (int)((((int64_t)job1 + 1) * ctas - 1) / total);
-                const unsigned n = (unsigned)(c1 - c0 + 1);
-                if (tid == 0) {
-                    __threadfence();
-                    s_last = atomicInc(a.counters + c0, n - 1u) == n - 1u;
-                    __threadfence();
+            if (!whole && tid == 0) {   // other CTAs work on this job too: the first and last of them are
+                int c0 = piece0, c1 = piece0 + pieces - 1;
+                if (!piece) {
+                    const int64_t job0 = start + kFixed, job1 = job0 + cur.nb - 1;   // its first and last pair on the axis
+                    c0 = n_pieces + (int)(((job0 + 1) * ctas - 1) / axis);
+                    c1 = n_pieces + (int)(((job1 + 1) * ctas - 1) / axis);
                 }
-                __syncthreads();
-                if (s_last) {
-                    for (int r = warp; r < ROWS; r += kWarps) {
-                        const int row = row0 + r, qi = row / a.group;
-                        if (qi >= a.L) continue;
-                        const float *src = a.part + r * (D + 2);
-                        auto at = [&](int c) { return src + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * ROWS * (D + 2); };
-                        float mx = -kNone;
-                        for (int c = c0 + lane; c <= c1; c += 32) mx = fmaxf(mx, __ldcg(at(c) + D));
-#pragma unroll
-                        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                        float sum[W32], lsum = 0.f;
-#pragma unroll
-                        for (int i = 0; i < W32; ++i) sum[i] = 0.f;
-#pragma unroll 4
-                        for (int c = c0; c <= c1; ++c) {
-                            const float f = ex2(__ldcg(at(c) + D) - mx);
-                            lsum = fmaf(f, __ldcg(at(c) + D + 1), lsum);
-#pragma unroll
-                            for (int i = 0; i < W32; ++i) sum[i] = fmaf(f, __ldcg(at(c) + i * 32 + lane), sum[i]);
-                        }
-                        const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-                        __nv_bfloat16 *o = a.o + cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr;
-#pragma unroll
-                        for (int i = 0; i < W32; ++i) o[i * 32 + lane] = __float2bfloat16_rn(lsum == 0.f ? 0.f : sum[i] * inv);
-                    }
-                }
+                int *to = s_pending[t0 == 0 ? 1 : 0];
+                to[0] = c0;
+                to[1] = c1;
+                to[2] = cur.b;
+                to[3] = cur.hk;
+                to[4] = row0;
             }
         }
+        first = false;
         start += cur.cost();
-        if (start < u_end) job_next<ROWS>(a, cur);
+        if (start < u_end) job_next<ROWS>(a, cur, share);
+    }
+
+    // ---- jobs that other CTAs work on too: whichever comes last adds the parts up
+    __syncthreads();
+    if (tid < 2) {
+        const int c0 = s_pending[tid][0];
+        s_last[tid] = 0;
+        if (c0 >= 0) {
+            const unsigned n = (unsigned)(s_pending[tid][1] - c0);
+            __threadfence();   // (fences are cumulative: this one stands for all that the barrier has ordered before it)
+            s_last[tid] = atomicInc(a.counters + c0, n) == n;
+            __threadfence();
+        }
+    }
+    __syncthreads();
+    for (int k = 0; k < 2; ++k) {
+        if (!s_last[k]) continue;
+        const int c0 = s_pending[k][0], c1 = s_pending[k][1], row0 = s_pending[k][4];
+        const int64_t b = s_pending[k][2], hk = s_pending[k][3];
+        for (int r = warp; r < ROWS; r += kWarps) {
+            const int row = row0 + r, qi = row / a.group;
+            if (qi >= a.L) continue;
+            const float *src = a.part + r * (D + 2);
+            auto at = [&](int c) { return src + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * ROWS * (D + 2); };
+            float mx = -kNone;
+            for (int c = c0 + lane; c <= c1; c += 32) mx = fmaxf(mx, __ldcg(at(c) + D));
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+            float sum[W32], lsum = 0.f;
+#pragma unroll
+            for (int i = 0; i < W32; ++i) sum[i] = 0.f;
+#pragma unroll 4
+            for (int c = c0; c <= c1; ++c) {
+                const float f = ex2(__ldcg(at(c) + D) - mx);
+                lsum = fmaf(f, __ldcg(at(c) + D + 1), lsum);
+#pragma unroll
+                for (int i = 0; i < W32; ++i) sum[i] = fmaf(f, __ldcg(at(c) + i * 32 + lane), sum[i]);
+            }
+            const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+            __nv_bfloat16 *o = a.o + b * a.o_sb + (hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr;
+#pragma unroll
+            for (int i = 0; i < W32; ++i) o[i * 32 + lane] = __float2bfloat16_rn(lsum == 0.f ? 0.f : sum[i] * inv);
+        }
     }
     if (dead) drain_copies();
 }
