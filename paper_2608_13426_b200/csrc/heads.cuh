@@ -3,6 +3,7 @@
 // Lane k of a row is turned against lane k +- rot/16 (pairs d, d + rot/2) or against itself (pairs 2 d, 2 d + 1).
 #pragma once
 #include "common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace rmm {
 
@@ -30,53 +31,90 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// Eight columns as they lie in memory, and as four pairs of fp32 numbers for the packed operations.
+template <typename T>
+struct Raw8 {
+    uint32_t w[sizeof(T) * 2];
+};
+using Eight = uint64_t[4];
+
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t both(float x) { return ptx::pack2(x, x); }
+
 // (plain loads: the rows may be written in place)
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, bool vec, float (&x)[8])
+__device__ __forceinline__ Raw8<T> load_raw(const T *p, bool vec)
 {
-    if constexpr (sizeof(T) == 2) {
-        if (vec) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(p);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    Raw8<T> r;
+    if (vec) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
         }
+    } else if constexpr (sizeof(T) == 2) {
+        const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = (uint32_t)h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
     } else {
-        if (vec) {
-            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-            x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = p[i];
-        }
+        for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(p[i]);
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> zero_raw()
+{
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) r.w[i] = 0u;
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen(const Raw8<T> &r, Eight &x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x[i] = sizeof(T) == 2 ? ptx::pack2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u))
+                              : ptx::pack2(__uint_as_float(r.w[(2 * i) % (sizeof(T) * 2)]), __uint_as_float(r.w[(2 * i + 1) % (sizeof(T) * 2)]));
+}
+__device__ __forceinline__ uint32_t narrow2(uint64_t v)
+{
+    float lo, hi;
+    ptx::unpack2(v, lo, hi);
+    return pack_bf16(lo, hi);
+}
+__device__ __forceinline__ void store_raw(__nv_bfloat16 *p, bool vec, const uint32_t (&w)[4])
+{
+    if (vec) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        unsigned short *h = reinterpret_cast<unsigned short *>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = (unsigned short)(w[i / 2] >> (16 * (i & 1)));
     }
 }
-
-template <typename T>
-__device__ __forceinline__ void store8(T *p, bool vec, const float (&x)[8])
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, bool vec, const Eight &x)
 {
-    if constexpr (sizeof(T) == 2) {
-        if (vec) {
-            *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-        } else {
+    const uint32_t w[4] = {narrow2(x[0]), narrow2(x[1]), narrow2(x[2]), narrow2(x[3])};
+    store_raw(p, vec, w);
+}
+__device__ __forceinline__ void store8(float *p, bool vec, const Eight &x)
+{
+    float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
-        }
+    for (int i = 0; i < 4; ++i) ptx::unpack2(x[i], v[2 * i], v[2 * i + 1]);
+    if (vec) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
-        if (vec) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = x[i];
-        }
+        for (int i = 0; i < 8; ++i) p[i] = v[i];
     }
 }
 
@@ -90,127 +128,199 @@ __device__ __forceinline__ float bf16_of_double(double z)
     return __bfloat162float(__float2bfloat16_rn(__uint_as_float(bits)));
 }
 
-// What a lane needs for every row of one position: its weights and its partner's, cosines, and sines with the sign of its side.
-struct RowLane {
-    float w[8], wp[8], c[8], s[8];
-    int partner;            // lane whose columns turn against mine
-    bool norm, rope, turns, self;
-};
-
-__device__ __forceinline__ void row_weights(RowLane &k, const void *weight, const RopeView &r, int col, int D)
+__device__ __forceinline__ void floats8(const float *p, float (&x)[8])
 {
-    k.norm = weight != nullptr;
-    k.rope = r.table != nullptr;
-    const int chunk = col / 8, half = r.rot / 16;
-    k.self = r.interleaved != 0;
-    k.turns = k.rope && chunk < 2 * half;
-    const int other = !k.turns || k.self ? chunk : (chunk < half ? chunk + half : chunk - half);
-    k.partner = ((int)threadIdx.x & 31) + other - chunk;
-    if (k.norm && col < D) {
-        if (r.weight_bf16) {
-            load8(static_cast<const __nv_bfloat16 *>(weight) + col, false, k.w);
-            load8(static_cast<const __nv_bfloat16 *>(weight) + 8 * other, false, k.wp);
-        } else {
-            load8(static_cast<const float *>(weight) + col, false, k.w);
-            load8(static_cast<const float *>(weight) + 8 * other, false, k.wp);
-        }
-    } else {
+    const Raw8<float> r = load_raw(p, reinterpret_cast<uintptr_t>(p) % 16 == 0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) k.w[i] = k.wp[i] = 1.f;
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.w[i]);
+}
+__device__ __forceinline__ void weights8(const void *weight, bool is_bf16, int col, float (&w)[8])
+{
+    if (is_bf16) {
+        const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(weight) + col;
+        const Raw8<__nv_bfloat16> r = load_raw(p, reinterpret_cast<uintptr_t>(p) % 16 == 0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = i & 1 ? __uint_as_float(r.w[i / 2] & 0xffff0000u) : bf16_bits(r.w[i / 2]);
+    } else {
+        floats8(static_cast<const float *>(weight) + col, w);
     }
 }
 
-__device__ __forceinline__ void row_angles(RowLane &k, const RopeView &r, int64_t position, int col)
+__device__ __forceinline__ int row_partner(const RopeView &r, int chunk)   // whose columns chunk's turn against
 {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        k.c[i] = 1.f;
-        k.s[i] = 0.f;
-    }
-    if (!k.turns) return;
+    const int half = r.rot / 16;
+    return chunk >= 2 * half || r.interleaved ? chunk : (chunk < half ? chunk + half : chunk - half);
+}
+// cosines, and sines with the sign of the side, of a turning lane's columns
+__device__ __forceinline__ void row_angles(const RopeView &r, int64_t position, int col, float (&c)[8], float (&s)[8])
+{
     const float *row = r.table + position * r.stride;
     const int half = r.rot / 2;
-    if (k.self) {
+    if (r.interleaved) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            k.c[i] = __ldg(row + (col + i) / 2);
-            k.s[i] = i & 1 ? __ldg(row + half + (col + i) / 2) : -__ldg(row + half + (col + i) / 2);
+        for (int i = 0; i < 8; i += 2) {
+            c[i] = c[i + 1] = row[(col + i) / 2];
+            s[i + 1] = row[half + (col + i) / 2];
+            s[i] = -s[i + 1];
         }
     } else {
         const int d = col < half ? col : col - half;
+        floats8(row + d, c);
+        floats8(row + half + d, s);
+        if (col < half)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            k.c[i] = __ldg(row + d + i);
-            k.s[i] = col < half ? -__ldg(row + half + d + i) : __ldg(row + half + d + i);
-        }
+            for (int i = 0; i < 8; ++i) s[i] = -s[i];
     }
 }
 
-// One row: z = (norm and rotation of x).  All lanes of the warp take part; lanes past the row's columns hold zeros.
-// ROUND: z is rounded to bf16 as the 64-bit result would be.  The fp32 chain is off by at most 2^-20 (|y c| + |y' s|): sum of up to
-// 256 squares in 8-element chains and 5 exchanges (14 roundings of 2^-24, half of it after the root), rsqrtf (4), two scalings,
-// product and sum (4).  Rows with a column that close to a border between two bf16 numbers (one in 20 or so) are done again in 64 bits.
-template <bool ROUND>
-__device__ __forceinline__ void norm_rope_row(const float (&x)[8], const RowLane &k, int lanes, int D, float eps, float (&z)[8])
+// What a lane needs for every row of one position: z = r (x a + x' b), x' being the columns that x is turned against.
+struct RowLane {
+    Eight a, b;             // weight times cosine; the partner's weight times the sine, with the sign of this side
+    int partner;            // lane of x'
+    bool norm, self, turns;
+};
+
+__device__ __forceinline__ void row_lane(RowLane &k, const void *weight, const RopeView &r, int64_t position, int col, int D)
 {
-    float r = 1.f;
-    if (k.norm) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-        for (int d = lanes >> 1; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        r = rsqrtf(sum / (float)D + eps);
-    }
-    float xp[8];
-    bool near = false;
-    if (k.rope && !k.self) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) xp[i] = __shfl_sync(0xffffffffu, x[i], k.partner);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) xp[i] = x[i ^ 1];
-    }
+    const int chunk = col / 8, other = row_partner(r, chunk);
+    k.norm = weight != nullptr;
+    k.self = r.table == nullptr || r.interleaved != 0;
+    k.turns = chunk < r.rot / 8;   // (rot is 0 without a table)
+    k.partner = ((int)threadIdx.x & 31) + other - chunk;
+    float a[8], b[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float y = x[i] * r * k.w[i];
+        a[i] = 1.f;
+        b[i] = k.turns ? 1.f : 0.f;
+    }
+    if (k.norm && col < D) {
+        weights8(weight, r.weight_bf16 != 0, col, a);
         if (k.turns) {
-            const float yp = xp[i] * r * (k.self ? k.w[i ^ 1] : k.wp[i]);
-            const float t = yp * k.s[i];
-            z[i] = fmaf(y, k.c[i], t);
-            if constexpr (ROUND) {
-                const uint32_t bits = __float_as_uint(z[i]);
-                const float off = fabsf(__uint_as_float(0x4b000000u | (bits & 0xffffu)) - 8421376.f);   // from the tie, units of fp32
-                near |= off * __uint_as_float(bits & 0x7f800000u) <= 8.f * fmaf(fabsf(y), fabsf(k.c[i]), fabsf(t));
-            }
-        } else {
-            z[i] = y;
-            if constexpr (ROUND) {
-                const uint32_t bits = __float_as_uint(y);
-                near |= k.norm && fabsf(__uint_as_float(0x4b000000u | (bits & 0xffffu)) - 8421376.f) <= 16.f;
-            }
+            float w[8];
+            weights8(weight, r.weight_bf16 != 0, 8 * other, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = k.self ? w[i ^ 1] : w[i];
         }
     }
-    if constexpr (ROUND) {
-        if (__any_sync(0xffffffffu, near)) {
-            double rd = 1.0;
-            if (k.norm) {
-                double sum = 0.0;
+    if (k.turns) {
+        float c[8], s[8];
+        row_angles(r, position, col, c, s);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum = fma((double)x[i], (double)x[i], sum);
-                for (int d = lanes >> 1; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                rd = 1.0 / sqrt(sum / (double)D + (double)eps);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double y = (double)x[i] * rd * (double)k.w[i];
-                const double yp = (double)xp[i] * rd * (double)(k.self ? k.w[i ^ 1] : k.wp[i]);
-                z[i] = bf16_of_double(k.turns ? fma(y, (double)k.c[i], yp * (double)k.s[i]) : y);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = __bfloat162float(__float2bfloat16_rn(z[i]));
+        for (int i = 0; i < 8; ++i) {
+            a[i] *= c[i];
+            b[i] *= s[i];
         }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        k.a[i] = ptx::pack2(a[2 * i], a[2 * i + 1]);
+        k.b[i] = ptx::pack2(b[2 * i], b[2 * i + 1]);
+    }
+}
+
+// x, x' of a row and what its norm scales with.  All lanes of the warp take part; lanes past the row's columns hold zeros.
+template <int LANES, typename T>
+__device__ __forceinline__ float row_scale(const Raw8<T> &raw, const RowLane &k, float inv_d, float eps, Eight &x, Eight &xp)
+{
+    widen(raw, x);
+    if (k.self) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xp[i] = x[i] >> 32 | x[i] << 32;
+    } else {
+        Raw8<T> other;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) * 2; ++i) other.w[i] = __shfl_sync(0xffffffffu, raw.w[i], k.partner);
+        widen(other, xp);
+    }
+    if (!k.norm) return 1.f;
+    uint64_t sum2 = fmul2(x[0], x[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) sum2 = ptx::ffma2(x[i], x[i], sum2);
+    float sum, hi;
+    ptx::unpack2(sum2, sum, hi);
+    sum += hi;
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return rsqrtf(fmaf(sum, inv_d, eps));
+}
+
+// A row in fp32.
+template <int LANES, typename T>
+__device__ __forceinline__ void norm_rope_row(const Raw8<T> &raw, const RowLane &k, float inv_d, float eps, Eight &z)
+{
+    Eight x, xp;
+    const uint64_t r = both(row_scale<LANES>(raw, k, inv_d, eps, x, xp));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = fmul2(ptx::ffma2(x[i], k.a[i], fmul2(xp[i], k.b[i])), r);
+}
+
+// The same row in 64 bits, rounded once to bf16.  (Out of the way: few rows come here.)
+template <int LANES>
+__device__ __noinline__ void norm_rope_row_64(const Eight &x2, const Eight &xp2, uint32_t *out, const void *weight, const RopeView &r, int64_t position, int col)
+{
+    constexpr int D = LANES * 8;
+    float x[8], xp[8], z[8];
+    for (int i = 0; i < 4; ++i) {
+        ptx::unpack2(x2[i], x[2 * i], x[2 * i + 1]);
+        ptx::unpack2(xp2[i], xp[2 * i], xp[2 * i + 1]);
+    }
+    double sum = 0.0, w = 1.0;
+    for (int i = 0; i < 8; ++i) sum = fma((double)x[i], (double)x[i], sum);
+    for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (weight != nullptr) w = 1.0 / sqrt(sum / (double)D + (double)r.eps);
+    const int chunk = col / 8, other = row_partner(r, chunk);
+    const bool turns = chunk < r.rot / 8;
+    float c[8], s[8];
+    if (turns) row_angles(r, position, col, c, s);
+    auto weight_of = [&](int d) -> double {
+        if (weight == nullptr) return 1.0;
+        return r.weight_bf16 ? (double)__bfloat162float(static_cast<const __nv_bfloat16 *>(weight)[d]) : (double)static_cast<const float *>(weight)[d];
+    };
+    for (int i = 0; i < 8; ++i) {
+        const double y = (double)x[i] * w * weight_of(col + i);
+        if (!turns) {
+            z[i] = bf16_of_double(y);
+            continue;
+        }
+        const double yp = (double)xp[i] * w * weight_of(r.interleaved ? col + (i ^ 1) : 8 * other + i);
+        z[i] = bf16_of_double(fma(y, (double)c[i], yp * (double)s[i]));
+    }
+    for (int i = 0; i < 4; ++i) out[i] = pack_bf16(z[2 * i], z[2 * i + 1]);
+}
+
+// A whole row (D = 8 LANES) rounded to bf16 as the 64-bit result would be.  The fp32 chain is off by at most
+// e = 2^-20 r (|x a| + |x' b|): sum of up to 256 squares in 4-element chains and 6 meetings, mean and eps (13 roundings of 2^-24, half
+// of that after the root), rsqrtf (4), a and b, two products, the scaling (4).  Where z - e and z + e round to different numbers, in one
+// row of 20 or so, the warp's rows are done again in 64 bits.
+template <int LANES, typename T>
+__device__ __forceinline__ void norm_rope_row_bf16(const Raw8<T> &raw, const RowLane &k, const void *weight, const RopeView &rope, int64_t position,
+                                                   int col, uint32_t (&out)[4])
+{
+    if (!k.norm && rope.table == nullptr) {   // nothing but the rounding
+        Eight x;
+        widen(raw, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = narrow2(x[i]);
+        return;
+    }
+    Eight x, xp;
+    const float r = row_scale<LANES>(raw, k, 1.f / (8 * LANES), rope.eps, x, xp), er = r * 9.5367431640625e-7f;
+    const uint64_t r2 = both(r);
+    uint32_t differ = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t t = fmul2(xp[i], k.b[i]), z = fmul2(ptx::ffma2(x[i], k.a[i], t), r2);
+        float x0, x1, a0, a1, t0, t1, z0, z1;
+        ptx::unpack2(x[i], x0, x1);
+        ptx::unpack2(k.a[i], a0, a1);
+        ptx::unpack2(t, t0, t1);
+        ptx::unpack2(z, z0, z1);
+        const float s0 = fmaf(fabsf(x0), fabsf(a0), fabsf(t0)), s1 = fmaf(fabsf(x1), fabsf(a1), fabsf(t1));
+        out[i] = pack_bf16(fmaf(s0, er, z0), fmaf(s1, er, z1));
+        differ |= out[i] ^ pack_bf16(fmaf(s0, -er, z0), fmaf(s1, -er, z1));
+    }
+    // (a sign's difference alone is a zero's)
+    if (__any_sync(0xffffffffu, differ != 0)) norm_rope_row_64<LANES>(x, xp, out, weight, rope, position, col);
 }
 
 int launch_norm_rope(const HeadRows (&rows)[2], int in_bf16, int out_bf16, const RopeView &rope, int64_t B, int64_t L, int64_t D, int *status,

@@ -20,138 +20,230 @@ struct CacheArgs {
     RopeView rope;
     int64_t groups;             // groups of neighbouring tokens of one sequence, per sequence
     int64_t B, L;
-    int D, lanes, heads_each;   // lanes of a row; heads of a warp
-    int head_groups;
+    int heads_each, head_groups;   // heads of a warp
     int *status;
 };
 
-struct Quantised {
-    uint32_t codes, pair;
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// Eight bf16 columns a lane, eight lanes a step: codes as whole numbers n, step and least value.
+// n is the nearest to the exact quotient (x - m) / s: a product by the reciprocal is off by less than 2^-18, and the exact remainder
+// x - m - n s says where it went to the wrong side of a half or met one (which goes to the even code).
+__device__ __forceinline__ void quantise8(const uint32_t (&w)[4], Eight &n, float &s, float &m)
+{
+    // least and (negated) largest value, side by side
+    const uint32_t lo2 = min_bf16x2(min_bf16x2(w[0], w[1]), min_bf16x2(w[2], w[3])), hi2 = max_bf16x2(max_bf16x2(w[0], w[1]), max_bf16x2(w[2], w[3]));
+    uint32_t ends = min_bf16x2(__byte_perm(lo2, hi2 ^ 0x80008000u, 0x5410), __byte_perm(lo2, hi2 ^ 0x80008000u, 0x7632));
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) ends = min_bf16x2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
+    m = bf16_bits(ends);
+    const float hi = -__uint_as_float(ends & 0xffff0000u);
+    s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, m), 15.f)));
+    const bool tiny = s < 7.5e-37f;   // too small for a reciprocal
+    const float half = 0.5f * s;
+    const uint64_t inv = both(s > 0.f ? __fdividef(1.f, s) : 0.f), magic = both(12582912.f), minus = both(-12582912.f), step = both(-s), least = both(-m);
+    Eight x;
+    widen(Raw8<__nv_bfloat16>{w[0], w[1], w[2], w[3]}, x);
+    bool near = tiny;
+    float e[8], a[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t off = ptx::fadd2(x[i], least);
+        n[i] = ptx::fadd2(ptx::ffma2(off, inv, magic), minus);   // to the nearest whole number
+        ptx::unpack2(off, a[2 * i], a[2 * i + 1]);
+        ptx::unpack2(ptx::ffma2(n[i], step, off), e[2 * i], e[2 * i + 1]);
+        near |= fabsf(e[2 * i]) >= half || fabsf(e[2 * i + 1]) >= half;
+    }
+    if (near && s > 0.f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float v[2];
+            ptx::unpack2(n[i], v[0], v[1]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float r = fabsf(e[2 * i + c]);
+                if (tiny) v[c] = rintf(__fdiv_rn(a[2 * i + c], s));
+                else if (r > half || (r == half && ((int)v[c] & 1))) v[c] += e[2 * i + c] > 0.f ? 1.f : -1.f;
+            }
+            n[i] = ptx::pack2(v[0], v[1]);
+        }
+    }
+    if (s == 0.f)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] = 0;
+}
+
+// (codes above 15, by the step's rounding, are 15)
+__device__ __forceinline__ uint32_t pack_codes(Eight &n)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        ptx::unpack2(n[i], v[2 * i], v[2 * i + 1]);
+        v[2 * i] = fminf(v[2 * i], 15.f);
+        v[2 * i + 1] = fminf(v[2 * i + 1], 15.f);
+        n[i] = ptx::pack2(v[2 * i], v[2 * i + 1]);
+    }
+    // four at a time are a whole number below 2^16
+    const float l = fmaf(fmaf(fmaf(v[3], 16.f, v[2]), 16.f, v[1]), 16.f, v[0]), h = fmaf(fmaf(fmaf(v[7], 16.f, v[6]), 16.f, v[5]), 16.f, v[4]);
+    return __byte_perm(__float_as_uint(l + 8388608.f), __float_as_uint(h + 8388608.f), 0x5410);
+}
+__device__ __forceinline__ uint32_t pack_pair(float s, float m) { return __byte_perm(__float_as_uint(s), __float_as_uint(m), 0x7632); }
+
+__device__ __forceinline__ void dequantise8(uint32_t codes, uint32_t pair, Eight &x)
+{
+    const uint64_t s = both(bf16_bits(pair)), m = both(__uint_as_float(pair & 0xffff0000u));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = ptx::ffma2(s, ptx::pack2((float)(codes >> (8 * i) & 15u), (float)(codes >> (8 * i + 4) & 15u)), m);
+}
+
+// Which token a lane's row is, and where it lies.
+template <int LANES>
+struct Place {
+    int64_t b, i, at;   // sequence, row of the call, token of the sequence
+    int h0, h1, col, t;
+    bool row, live;     // a row of the call; one that is a token
+    uint8_t *base;      // its block of head h0, or NULL
+    __device__ __forceinline__ bool find(const CacheArgs &a, int64_t unit, int64_t table_rows)
+    {
+        const int lane = threadIdx.x & 31;
+        b = unit / a.groups;
+        i = (unit - b * a.groups) * (32 / LANES) + lane / LANES;
+        col = (lane & (LANES - 1)) * 8;
+        h0 = (int)(blockIdx.x % a.head_groups) * a.heads_each;
+        h1 = min(a.k.heads, h0 + a.heads_each);
+        int len, rows;
+        kv4::sequence(a.cache, b, len, rows, a.status);
+        at = (int64_t)len - rows + i;
+        row = i < a.L;
+        live = row && i < rows;
+        if (live && (at < 0 || at >= table_rows)) {
+            atomicExch(a.status, (int)RMM_ERR_BOUNDS);
+            live = false;
+        }
+        base = live ? kv4::block_of(a.cache, b, h0, at / kv4::kBlock, LANES * 8, a.status) : nullptr;
+        t = (int)(at & (kv4::kBlock - 1));
+        return live;
+    }
 };
 
-__device__ __forceinline__ Quantised quantise8(const float (&x)[8])
+template <typename TI, bool HELD, int LANES>
+__global__ void __launch_bounds__(kWarps * 32, 2) kv4_append_kernel(const __grid_constant__ CacheArgs a)
 {
-    float lo = x[0], hi = x[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-    }
-#pragma unroll
-    for (int d = 4; d > 0; d >>= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-    }
-    const uint32_t step = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f)));
-    const float s = bf16_bits(step);
-    Quantised q;
-    q.codes = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float n = s > 0.f ? fminf(rintf(__fdiv_rn(__fsub_rn(x[i], lo), s)), 15.f) : 0.f;
-        q.codes |= (uint32_t)n << (4 * i);
-    }
-    q.pair = step | (__float_as_uint(lo) & 0xffff0000u);
-    return q;
-}
-
-__device__ __forceinline__ void dequantise8(uint32_t codes, uint32_t pair, float (&x)[8])
-{
-    const float s = bf16_bits(pair & 0xffffu), m = __uint_as_float(pair & 0xffff0000u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fmaf(s, (float)(codes >> (4 * i) & 15u), m);
-}
-
-template <typename TI, bool HELD>
-__global__ void __launch_bounds__(kWarps * 32) kv4_append_kernel(const __grid_constant__ CacheArgs a)
-{
+    constexpr int D = LANES * 8;
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 32 / a.lanes, D = a.D;
-    const int64_t unit = (int64_t)(blockIdx.x / a.head_groups) * kWarps + warp;
+    const int64_t unit = (int64_t)(blockIdx.x / a.head_groups) * kWarps + (threadIdx.x >> 5);
     if (unit >= a.B * a.groups) return;
-    const int64_t b = unit / a.groups, i = (unit - b * a.groups) * per + lane / a.lanes;
-    const int col = (lane & (a.lanes - 1)) * 8, chunk = col / 8;
-    const int h0 = (int)(blockIdx.x % a.head_groups) * a.heads_each, h1 = min(a.k.heads, h0 + a.heads_each);
-    int len, rows;
-    kv4::sequence(a.cache, b, len, rows, a.status);
-    const int64_t at = (int64_t)len - rows + i;
-    const bool row = i < a.L;
-    bool live = row && i < rows;
-    if (live && (at < 0 || (a.rope.table != nullptr && at >= a.rope.rows))) {
-        atomicExch(a.status, (int)RMM_ERR_BOUNDS);
-        live = false;
+    Place<LANES> p;
+    const bool live = p.find(a, unit, a.rope.table != nullptr ? a.rope.rows : INT64_MAX);
+    const int64_t position = live ? p.at : 0;
+    const TI *ks = static_cast<const TI *>(a.k.src) + p.b * a.k.s_b + p.i * a.k.s_r + p.h0 * a.k.s_h + p.col;
+    const TI *vs = static_cast<const TI *>(a.v.src) + p.b * a.v.s_b + p.i * a.v.s_r + p.h0 * a.v.s_h + p.col;
+    const bool k_vec = a.k.vec_in != 0, v_vec = a.v.vec_in != 0;
+    Raw8<TI> x = zero_raw<TI>(), v = x, x_ahead = x, v_ahead = x;
+    if (live) {
+        x = load_raw(ks, k_vec);
+        v = load_raw(vs, v_vec);
     }
-    uint8_t *base = live ? kv4::block_of(a.cache, b, h0, at / kv4::kBlock, D, a.status) : nullptr;
-    const int t = (int)(at & (kv4::kBlock - 1));
     RowLane k;
-    row_weights(k, a.k.weight, a.rope, col, D);
-    row_angles(k, a.rope, live ? at : 0, col);
-    const TI *ks = static_cast<const TI *>(a.k.src) + b * a.k.s_b + i * a.k.s_r + col;
-    const TI *vs = static_cast<const TI *>(a.v.src) + b * a.v.s_b + i * a.v.s_r + col;
-    for (int h = h0; h < h1; ++h) {
-        float x[8], v[8], z[8];
-        if (live) {
-            load8(ks + h * a.k.s_h, a.k.vec_in != 0, x);
-            load8(vs + h * a.v.s_h, a.v.vec_in != 0, v);
+    row_lane(k, a.k.weight, a.rope, position, p.col, D);
+    const int chunk = p.col / 8;
+    uint32_t *base = reinterpret_cast<uint32_t *>(p.base);
+    const int key = kv4::key_word(D, p.t, chunk), value = kv4::value_word(D, p.t, chunk), pair = kv4::key_pair_word(D, p.t, chunk >> 3);
+    __nv_bfloat16 *kh = nullptr, *vh = nullptr;
+    if (HELD) {
+        kh = static_cast<__nv_bfloat16 *>(a.k.dst) + p.b * a.k.d_b + p.i * a.k.d_r + p.h0 * a.k.d_h + p.col;
+        vh = static_cast<__nv_bfloat16 *>(a.v.dst) + p.b * a.v.d_b + p.i * a.v.d_r + p.h0 * a.v.d_h + p.col;
+    }
+    for (int h = p.h0; h < p.h1; ++h) {
+        if (live && h + 1 < p.h1) {   // under way while this head is worked on
+            ks += a.k.s_h;
+            vs += a.v.s_h;
+            x_ahead = load_raw(ks, k_vec);
+            v_ahead = load_raw(vs, v_vec);
+        }
+        uint32_t zk[4], zv[4];
+        norm_rope_row_bf16<LANES>(x, k, a.k.weight, a.rope, position, p.col, zk);
+        if constexpr (sizeof(TI) == 2) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) zv[e] = v.w[e];
         } else {
+            Eight y;
+            widen(v, y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = v[e] = 0.f;
+            for (int e = 0; e < 4; ++e) zv[e] = narrow2(y[e]);
         }
-        norm_rope_row<true>(x, k, a.lanes, D, a.rope.eps, z);
-        if constexpr (sizeof(TI) == 4) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = __bfloat162float(__float2bfloat16_rn(v[e]));
-        }
-        const Quantised qk = quantise8(z), qv = quantise8(v);
+        Eight nk, nv;
+        float sk, sv, mk, mv;
+        quantise8(zk, nk, sk, mk);
+        quantise8(zv, nv, sv, mv);
+        const uint32_t ck = pack_codes(nk), cv = pack_codes(nv);
         if (base != nullptr) {
-            uint32_t *w = reinterpret_cast<uint32_t *>(base + (h - h0) * a.cache.head_stride);
-            w[kv4::key_word(D, t, chunk)] = qk.codes;
-            w[kv4::value_word(D, t, chunk)] = qv.codes;
+            base[key] = ck;
+            base[value] = cv;
             if ((chunk & 7) == 0) {
-                w[kv4::key_pair_word(D, t, chunk >> 3)] = qk.pair;
-                w[kv4::value_pair_word(D, t, chunk >> 3)] = qv.pair;
+                base[pair] = pack_pair(sk, mk);
+                base[pair + D / 4] = pack_pair(sv, mv);
             }
+            base += a.cache.head_stride / 4;
         }
         if constexpr (HELD) {
-            if (row) {
-                dequantise8(qk.codes, qk.pair, x);   // (rows that are none: zeros)
-                dequantise8(qv.codes, qv.pair, v);
-                store8(static_cast<__nv_bfloat16 *>(a.k.dst) + b * a.k.d_b + h * a.k.d_h + i * a.k.d_r + col, a.k.vec_out != 0, x);
-                store8(static_cast<__nv_bfloat16 *>(a.v.dst) + b * a.v.d_b + h * a.v.d_h + i * a.v.d_r + col, a.v.vec_out != 0, v);
+            if (p.row) {   // (rows that are none: zeros)
+                const uint64_t sk2 = both(sk), sv2 = both(sv), mk2 = both(mk), mv2 = both(mv);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    nk[e] = ptx::ffma2(sk2, nk[e], mk2);
+                    nv[e] = ptx::ffma2(sv2, nv[e], mv2);
+                }
+                store8(kh, a.k.vec_out != 0, nk);
+                store8(vh, a.v.vec_out != 0, nv);
             }
+            kh += a.k.d_h;
+            vh += a.v.d_h;
         }
+        x = x_ahead;
+        v = v_ahead;
     }
 }
 
-template <typename TO>
+template <typename TO, int LANES>
 __global__ void __launch_bounds__(kWarps * 32) kv4_read_kernel(const __grid_constant__ CacheArgs a)
 {
+    constexpr int D = LANES * 8;
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 32 / a.lanes, D = a.D;
-    const int64_t unit = (int64_t)(blockIdx.x / a.head_groups) * kWarps + warp;
+    const int64_t unit = (int64_t)(blockIdx.x / a.head_groups) * kWarps + (threadIdx.x >> 5);
     if (unit >= a.B * a.groups) return;
-    const int64_t b = unit / a.groups, i = (unit - b * a.groups) * per + lane / a.lanes;
-    const int col = (lane & (a.lanes - 1)) * 8, chunk = col / 8;
-    const int h0 = (int)(blockIdx.x % a.head_groups) * a.heads_each, h1 = min(a.k.heads, h0 + a.heads_each);
-    int len, rows;
-    kv4::sequence(a.cache, b, len, rows, a.status);
-    if (i >= a.L) return;
-    const int64_t at = (int64_t)len - rows + i;
-    const uint8_t *base = nullptr;
-    if (i < rows) {
-        if (at < 0) atomicExch(a.status, (int)RMM_ERR_BOUNDS);
-        else base = kv4::block_of(a.cache, b, h0, at / kv4::kBlock, D, a.status);
-    }
-    const int t = (int)(at & (kv4::kBlock - 1));
-    for (int h = h0; h < h1; ++h) {
-        float k[8] = {}, v[8] = {};
+    Place<LANES> p;
+    p.find(a, unit, INT64_MAX);
+    if (!p.row) return;
+    const int chunk = p.col / 8;
+    const uint32_t *base = reinterpret_cast<const uint32_t *>(p.base);
+    const int key = kv4::key_word(D, p.t, chunk), value = kv4::value_word(D, p.t, chunk), pair = kv4::key_pair_word(D, p.t, chunk >> 3);
+    TO *kh = static_cast<TO *>(a.k.dst) + p.b * a.k.d_b + p.i * a.k.d_r + p.h0 * a.k.d_h + p.col;
+    TO *vh = static_cast<TO *>(a.v.dst) + p.b * a.v.d_b + p.i * a.v.d_r + p.h0 * a.v.d_h + p.col;
+#pragma unroll 2
+    for (int h = p.h0; h < p.h1; ++h) {
+        Eight k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
         if (base != nullptr) {
-            const uint32_t *w = reinterpret_cast<const uint32_t *>(base + (h - h0) * a.cache.head_stride);
-            dequantise8(w[kv4::key_word(D, t, chunk)], w[kv4::key_pair_word(D, t, chunk >> 3)], k);
-            dequantise8(w[kv4::value_word(D, t, chunk)], w[kv4::value_pair_word(D, t, chunk >> 3)], v);
+            dequantise8(base[key], base[pair], k);
+            dequantise8(base[value], base[pair + D / 4], v);
+            base += a.cache.head_stride / 4;
         }
-        store8(static_cast<TO *>(a.k.dst) + b * a.k.d_b + h * a.k.d_h + i * a.k.d_r + col, a.k.vec_out != 0, k);
-        store8(static_cast<TO *>(a.v.dst) + b * a.v.d_b + h * a.v.d_h + i * a.v.d_r + col, a.v.vec_out != 0, v);
+        store8(kh, a.k.vec_out != 0, k);
+        store8(vh, a.v.vec_out != 0, v);
+        kh += a.k.d_h;
+        vh += a.v.d_h;
     }
 }
 
@@ -162,9 +254,7 @@ int fill(CacheArgs &a, const HeadRows &K, const HeadRows &V, const kv4::View &ca
     a.cache = cache;
     a.B = B;
     a.L = L;
-    a.D = (int)D;
-    a.lanes = (int)D / 8;
-    a.groups = ceil_div(L, 32 / a.lanes);
+    a.groups = ceil_div(L, 256 / D);
     a.status = status;
     // All heads of a token by one warp, where that still leaves sixteen warps an SM
     const int64_t token_blocks = ceil_div(B * a.groups, kWarps), want = ceil_div((int64_t)sm_count() * 2, token_blocks);
@@ -173,6 +263,18 @@ int fill(CacheArgs &a, const HeadRows &K, const HeadRows &V, const kv4::View &ca
     a.head_groups = (int)ceil_div(K.heads, a.heads_each);
     blocks = token_blocks * a.head_groups;
     return blocks > INT32_MAX ? fail(RMM_ERR_UNSUPPORTED, "kv4: more than 2^31 blocks of rows") : (int)RMM_OK;
+}
+
+using Kernel = void (*)(CacheArgs);
+template <typename TI, bool HELD>
+Kernel append_kernel(int64_t D)
+{
+    return D == 64 ? kv4_append_kernel<TI, HELD, 8> : (D == 128 ? kv4_append_kernel<TI, HELD, 16> : kv4_append_kernel<TI, HELD, 32>);
+}
+template <typename TO>
+Kernel read_kernel(int64_t D)
+{
+    return D == 64 ? kv4_read_kernel<TO, 8> : (D == 128 ? kv4_read_kernel<TO, 16> : kv4_read_kernel<TO, 32>);
 }
 
 }  // namespace
@@ -185,8 +287,8 @@ int launch_kv4_append(const HeadRows &K, const HeadRows &V, const kv4::View &cac
     a.rope = rope;
     if (int rc = fill(a, K, V, cache, B, L, D, status, blocks)) return rc;
     const bool held = K.dst != nullptr;
-    auto kern = in_bf16 ? (held ? kv4_append_kernel<__nv_bfloat16, true> : kv4_append_kernel<__nv_bfloat16, false>)
-                        : (held ? kv4_append_kernel<float, true> : kv4_append_kernel<float, false>);
+    const Kernel kern = in_bf16 ? (held ? append_kernel<__nv_bfloat16, true>(D) : append_kernel<__nv_bfloat16, false>(D))
+                                : (held ? append_kernel<float, true>(D) : append_kernel<float, false>(D));
     prof_begin("kv4_append_kernel", stream);
     launch_kernel(kern, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, a);
     return check_launch("kv4_append_kernel", stream);
@@ -198,7 +300,7 @@ int launch_kv4_read(const HeadRows &K, const HeadRows &V, const kv4::View &cache
     CacheArgs a = {};
     int64_t blocks;
     if (int rc = fill(a, K, V, cache, B, L, D, status, blocks)) return rc;
-    auto kern = out_bf16 ? kv4_read_kernel<__nv_bfloat16> : kv4_read_kernel<float>;
+    const Kernel kern = out_bf16 ? read_kernel<__nv_bfloat16>(D) : read_kernel<float>(D);
     prof_begin("kv4_read_kernel", stream);
     launch_kernel(kern, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, a);
     return check_launch("kv4_read_kernel", stream);

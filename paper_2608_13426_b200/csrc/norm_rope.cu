@@ -9,56 +9,80 @@
 namespace rmm {
 namespace {
 
-constexpr int kWarps = 8, kTurns = 4;   // warps of a block: neighbouring tokens; rows of a lane
+constexpr int kWarps = 8;   // of a block: neighbouring tokens
 
 struct NormRopeArgs {
     HeadRows rows[2];
     RopeView rope;
     int64_t tokens, L;
-    int D, lanes, groups[2];   // lanes of a row; warps that share a token's heads
+    int D, rounds, groups[2];   // kTurns rows a lane, so many times; warps that share a token's heads
+    float inv_d;
     int *status;
 };
 
-template <typename TI, typename TO>
-__global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const __grid_constant__ NormRopeArgs a)
+template <typename TI>
+constexpr int kTurns = sizeof(TI) == 2 ? 4 : 2;   // rows that a lane asks for at a time: 64 bytes, twice over
+
+template <typename TI, typename TO, int LANES>
+__global__ void __launch_bounds__(kWarps * 32, 3) norm_rope_kernel(const __grid_constant__ NormRopeArgs a)
 {
+    constexpr int T = kTurns<TI>, PER = 32 / LANES;
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 32 / a.lanes;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int all = a.groups[0] + a.groups[1], g = blockIdx.x % all;
     const int64_t token = (int64_t)(blockIdx.x / all) * kWarps + warp;
     if (token >= a.tokens) return;
     const bool second = g >= a.groups[0];
     const HeadRows &h = a.rows[second];
     const int64_t b = token / a.L, i = token - b * a.L;
-    const int first = (second ? g - a.groups[0] : g) * per * kTurns + lane / a.lanes, col = (lane & (a.lanes - 1)) * 8;
+    const int first = (second ? g - a.groups[0] : g) * PER * T * a.rounds, mine = first + lane / LANES, col = (lane & (LANES - 1)) * 8;
+    const int end = min(h.heads, first + PER * T * a.rounds);
     const int64_t position = a.rope.positions != nullptr ? a.rope.positions[b * a.rope.p_b + i * a.rope.p_r] : i;
     if (a.rope.table != nullptr && (position < 0 || position >= a.rope.rows)) {   // such a row is not written
         if (lane == 0) atomicExch(a.status, (int)RMM_ERR_BOUNDS);
         return;
     }
-    const TI *src = static_cast<const TI *>(h.src) + b * h.s_b + i * h.s_r + col;
-    TO *dst = static_cast<TO *>(h.dst) + b * h.d_b + i * h.d_r + col;
-    float x[kTurns][8];
+    const bool in_row = col < a.D, vec_in = h.vec_in != 0, vec_out = h.vec_out != 0;
+    const int64_t s_step = PER * h.s_h, d_step = PER * h.d_h;
+    const TI *src = static_cast<const TI *>(h.src) + b * h.s_b + i * h.s_r + mine * h.s_h + col;
+    TO *dst = static_cast<TO *>(h.dst) + b * h.d_b + i * h.d_r + mine * h.d_h + col;
+    Raw8<TI> x[T], ahead[T];
+    auto load = [&](int head0, Raw8<TI> (&to)[T]) {
 #pragma unroll
-    for (int t = 0; t < kTurns; ++t) {
-        const int head = first + t * per;
-        if (head < h.heads && col < a.D) {
-            load8(src + head * h.s_h, h.vec_in != 0, x[t]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[t][e] = 0.f;
+        for (int t = 0; t < T; ++t) {
+            to[t] = head0 + t * PER < end && in_row ? load_raw(src, vec_in) : zero_raw<TI>();
+            src += s_step;
         }
-    }
+    };
+    load(mine, x);
     RowLane k;
-    row_weights(k, h.weight, a.rope, col, a.D);
-    row_angles(k, a.rope, position, col);
+    row_lane(k, h.weight, a.rope, position, col, a.D);
+    for (int head0 = first; head0 < end; head0 += PER * T) {
+        load(head0 + lane / LANES + PER * T, ahead);
 #pragma unroll
-    for (int t = 0; t < kTurns; ++t) {
-        float z[8];
-        norm_rope_row<false>(x[t], k, a.lanes, a.D, a.rope.eps, z);
-        const int head = first + t * per;
-        if (head < h.heads && col < a.D) store8(dst + head * h.d_h, h.vec_out != 0, z);
+        for (int t = 0; t < T; ++t) {
+            Eight z;
+            norm_rope_row<LANES>(x[t], k, a.inv_d, a.rope.eps, z);
+            if (head0 + lane / LANES + t * PER < end && in_row) store8(dst, vec_out, z);
+            dst += d_step;
+        }
+#pragma unroll
+        for (int t = 0; t < T; ++t) x[t] = ahead[t];
     }
+}
+
+template <typename TI, typename TO>
+int launch_lanes(const NormRopeArgs &a, int lanes, int64_t blocks, cudaStream_t stream)
+{
+    using Kernel = void (*)(NormRopeArgs);
+    const Kernel kern = lanes == 2    ? norm_rope_kernel<TI, TO, 2>
+                        : lanes == 4  ? norm_rope_kernel<TI, TO, 4>
+                        : lanes == 8  ? norm_rope_kernel<TI, TO, 8>
+                        : lanes == 16 ? norm_rope_kernel<TI, TO, 16>
+                                      : norm_rope_kernel<TI, TO, 32>;
+    prof_begin("norm_rope_kernel", stream);
+    launch_kernel(kern, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, a);
+    return check_launch("norm_rope_kernel", stream);
 }
 
 }  // namespace
@@ -73,16 +97,20 @@ int launch_norm_rope(const HeadRows (&rows)[2], int in_bf16, int out_bf16, const
     a.tokens = B * L;
     a.L = L;
     a.D = (int)D;
-    for (a.lanes = 2; a.lanes * 8 < D;) a.lanes *= 2;
-    for (int i = 0; i < 2; ++i) a.groups[i] = (int)ceil_div(rows[i].heads, 32 / a.lanes * kTurns);
+    a.inv_d = 1.f / (float)D;
     a.status = status;
+    int lanes = 2;
+    while (lanes * 8 < D) lanes *= 2;
+    const int64_t at_once = 32 / lanes * (in_bf16 ? kTurns<__nv_bfloat16> : kTurns<float>);
+    // A warp takes up to four times as many heads of its token as it asks for at once, as long as that leaves sixteen warps an SM
+    const int64_t most = rows[0].heads > rows[1].heads ? rows[0].heads : rows[1].heads;
+    for (a.rounds = 4; a.rounds > 1; a.rounds /= 2)
+        if (at_once * (a.rounds / 2) < most && a.tokens * ceil_div(most, at_once * a.rounds) >= (int64_t)sm_count() * 16) break;
+    for (int i = 0; i < 2; ++i) a.groups[i] = (int)ceil_div(rows[i].heads, at_once * a.rounds);
     const int64_t blocks = ceil_div(a.tokens, kWarps) * (a.groups[0] + a.groups[1]);
     if (blocks > INT32_MAX) return fail(RMM_ERR_UNSUPPORTED, "qk_norm_rope: more than 2^31 blocks of rows");
-    auto kern = in_bf16 ? (out_bf16 ? norm_rope_kernel<__nv_bfloat16, __nv_bfloat16> : norm_rope_kernel<__nv_bfloat16, float>)
-                        : (out_bf16 ? norm_rope_kernel<float, __nv_bfloat16> : norm_rope_kernel<float, float>);
-    prof_begin("norm_rope_kernel", stream);
-    launch_kernel(kern, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, a);
-    return check_launch("norm_rope_kernel", stream);
+    if (in_bf16) return out_bf16 ? launch_lanes<__nv_bfloat16, __nv_bfloat16>(a, lanes, blocks, stream) : launch_lanes<__nv_bfloat16, float>(a, lanes, blocks, stream);
+    return out_bf16 ? launch_lanes<float, __nv_bfloat16>(a, lanes, blocks, stream) : launch_lanes<float, float>(a, lanes, blocks, stream);
 }
 
 }  // namespace rmm
