@@ -1,5 +1,6 @@
-"""Thin binding of librmm_b200.so: argument marshalling only, by ctypes and, for the plain form of the two calls that
-the host can bound (rmm_product, rmm_reduced_attn), by a small native module (csrc/marshal.c).
+"""Thin binding of librmm_b200.so: argument marshalling only, by ctypes and, for the plain form of the calls that
+the host can bound (rmm_product, rmm_reduced_attn, those on rows of heads and the 4-bit cache), by a small native module
+(csrc/marshal.c).
 
 Every function has the name of the C entry point it calls (include/rmm.h).  Tensors are torch CUDA
 tensors used as plain device memory; the current torch stream is the launch stream.  Workspaces are
@@ -187,7 +188,7 @@ def _native():
         if not os.path.exists(MARSHAL_PATH):
             return None
         from . import rmm_marshal
-        rmm_marshal.init(L._name, (torch.Tensor, torch.nn.Parameter), (torch.bfloat16, torch.float32, torch.int32),
+        rmm_marshal.init(L._name, (torch.Tensor, torch.nn.Parameter), (torch.bfloat16, torch.float32, torch.int32, torch.uint8),
                          (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice), globals())
         rmm_marshal.set_poison(_poison)
         _marshal = rmm_marshal
@@ -586,7 +587,6 @@ def rmm_rope_table(positions: int, rot: int, base: float = 10000.0, device=None)
     return torch.cat([angles.cos(), angles.sin()], 1).float()
 
 
-@_on_device
 def rmm_qk_norm_rope(Q: torch.Tensor, K: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
                      k_weight: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
                      eps: float = 1e-6, interleaved: bool = False, out_dtype: Optional[torch.dtype] = None, inplace: bool = False,
@@ -595,6 +595,15 @@ def rmm_qk_norm_rope(Q: torch.Tensor, K: Optional[torch.Tensor] = None, q_weight
     dim contiguous; weights [D] (None: that side is not normalised); rope fp32 [P, rot] (rmm_rope_table; None: no rotation);
     positions int32 [B, L] or [L] (None: row i is at position i).  Returns (Q', K'), or Q' without K: new contiguous tensors in
     out_dtype (the inputs' own if None), or with inplace the inputs themselves."""
+    if out_dtype is None and not inplace and ws is None and (native := _marshal or _native()) is not None:
+        done = native.norm_rope(Q, K, q_weight, k_weight, rope, positions, eps, interleaved)
+        if done is not None:
+            return done
+    return _qk_norm_rope(Q, K, q_weight, k_weight, rope, positions, eps, interleaved, out_dtype, inplace, ws)
+
+
+@_on_device
+def _qk_norm_rope(Q, K, q_weight, k_weight, rope, positions, eps, interleaved, out_dtype, inplace, ws):
     device = Q.device if isinstance(Q, torch.Tensor) else None
     q = _heads(Q, "Q", device)
     k = None if K is None else _heads(K, "K", device)
@@ -629,7 +638,6 @@ def rmm_kv4_pool(n_pages: int, Hkv: int, Dh: int, page: int = 64, device=None) -
     return torch.zeros(n_pages, Hkv, page // 16, 18 * Dh, dtype=torch.uint8, device="cuda" if device is None else device)
 
 
-@_on_device
 def rmm_kv4_append(K: torch.Tensor, V: torch.Tensor, pool: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor,
                    new_len: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
                    eps: float = 1e-6, interleaved: bool = False, want_values: bool = False, ws: Optional[torch.Tensor] = None):
@@ -637,6 +645,15 @@ def rmm_kv4_append(K: torch.Tensor, V: torch.Tensor, pool: torch.Tensor, pages: 
     pages int32 [B, max_pages] holds page numbers of `pool`; lengths int32 [B] counts each sequence's tokens with the new ones, which
     are the first new_len[b] rows (None: all L): row i becomes token lengths[b] - new_len[b] + i and is rotated at that position.
     With want_values returns (K', V') bf16 [B,Hkv,L,Dh]: what the cache holds for these rows (zeros behind new_len)."""
+    if ws is None and (native := _marshal or _native()) is not None:
+        done = native.kv4_append(K, V, pool, pages, lengths, new_len, k_weight, rope, eps, interleaved, want_values)
+        if done is not None:
+            return done or None
+    return _kv4_append(K, V, pool, pages, lengths, new_len, k_weight, rope, eps, interleaved, want_values, ws)
+
+
+@_on_device
+def _kv4_append(K, V, pool, pages, lengths, new_len, k_weight, rope, eps, interleaved, want_values, ws):
     device = K.device if isinstance(K, torch.Tensor) else None
     k, v = _heads(K, "K", device), _heads(V, "V", device)
     c = _kv4(pool, pages, lengths, new_len, device)
@@ -652,11 +669,19 @@ def rmm_kv4_append(K: torch.Tensor, V: torch.Tensor, pool: torch.Tensor, pages: 
     return (Ko, Vo) if want_values else None
 
 
-@_on_device
 def rmm_kv4_read(pool: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor, new_len: Optional[torch.Tensor] = None,
                  rows: int = 1, out_dtype: torch.dtype = torch.bfloat16, ws: Optional[torch.Tensor] = None):
     """(K, V) [B, Hkv, rows, Dh] of the last new_len[b] tokens of every sequence (None: of the last `rows`), zeros behind them; with
     new_len = lengths whole sequences.  What a long chunk's rmm_reduced_attn reads."""
+    if ws is None and (native := _marshal or _native()) is not None:
+        done = native.kv4_read(pool, pages, lengths, new_len, rows, out_dtype)
+        if done is not None:
+            return done
+    return _kv4_read(pool, pages, lengths, new_len, rows, out_dtype, ws)
+
+
+@_on_device
+def _kv4_read(pool, pages, lengths, new_len, rows, out_dtype, ws):
     device = pool.device if isinstance(pool, torch.Tensor) else None
     c = _kv4(pool, pages, lengths, new_len, device)
     K, V = (_out((c.B, c.Hkv, int(rows), c.Dh), out_dtype, pool) for _ in range(2))
@@ -666,13 +691,21 @@ def rmm_kv4_read(pool: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor,
     return K, V
 
 
-@_on_device
 def rmm_kv4_attn(Q: torch.Tensor, pool: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor, new_len: Optional[torch.Tensor] = None,
                  causal: bool = True, rho_d: float = 1.0, want_idx: bool = False, ws: Optional[torch.Tensor] = None):
     """Reduced attention of Q [B,Hq,L,Dh] bf16 over the paged 4-bit cache: rows i < new_len[b] (None: all L) are the last tokens of
     lengths[b]; causal rows see the tokens up to their own, the others all.  Returns O [B,Hq,L,Dh] bf16 (zeros where a row sees
     nothing, and behind new_len), or (O, idx_feat) with want_idx.  A call that is captured into a graph needs a `ws` of its own
     that lives as long as the graph, as do calls that may overlap."""
+    if ws is None and not want_idx and (native := _marshal or _native()) is not None:
+        done = native.kv4_attn(Q, pool, pages, lengths, new_len, causal, rho_d)
+        if done is not None:
+            return done
+    return _kv4_attn(Q, pool, pages, lengths, new_len, causal, rho_d, want_idx, ws)
+
+
+@_on_device
+def _kv4_attn(Q, pool, pages, lengths, new_len, causal, rho_d, want_idx, ws):
     device = Q.device if isinstance(Q, torch.Tensor) else None
     q = _heads(Q, "Q", device)
     c = _kv4(pool, pages, lengths, new_len, device)

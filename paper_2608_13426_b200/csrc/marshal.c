@@ -1,6 +1,6 @@
-/* Argument marshalling of the two calls whose launches are short enough for the host to bound them, rmm_product and
- * rmm_reduced_attn, as one native call each: reading three or four tensors, asking for the workspace size and calling the library
- * through ctypes took about as long as the GPU needs for a small product twice over.
+/* Argument marshalling of the calls whose launches are short enough for the host to bound them (rmm_product, rmm_reduced_attn, and
+ * those on rows of heads and the 4-bit cache) as one native call each: reading three or four tensors, asking for the workspace size
+ * and calling the library through ctypes took about as long as the GPU needs for a small product twice over.
  *
  * Only the plain form is taken (torch.Tensor or Parameter, no buffer passed in).  Whatever else it meets, and every
  * argument that would be refused, is answered with None: the caller's Python code then does the whole call, and raises what
@@ -12,7 +12,7 @@
 #include "rmm.h"
 
 static PyTypeObject *type_tensor, *type_parameter;
-static PyObject *dt_bf16, *dt_f32, *dt_i32;
+static PyObject *dt_bf16, *dt_f32, *dt_i32, *dt_u8;
 static PyObject *fn_stream, *fn_device, *names;   /* names: the Python module's, looked up at every call */
 static PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_new_empty, *s_get_device, *s_numel, *s_device, *s_cuda, *s_ws_cache, *s_workspace, *s_check, *s_out, *kw_dtype;
 static int poison;
@@ -24,6 +24,11 @@ static size_t (*p_gemm_ws)(const rmm_mat_t *, const rmm_mat_t *, int64_t, const 
 static int (*p_product)(const rmm_mat_t *, const rmm_mat_t *, double, int64_t, float, const rmm_mat_t *, int32_t *, float *, void *, size_t, void *);
 static size_t (*p_attn_ws)(const rmm_attn_desc_t *);
 static int (*p_attn)(const rmm_attn_desc_t *, const void *, const void *, const void *, void *, int32_t *, int32_t *, void *, size_t, void *);
+static int (*p_norm_rope)(const rmm_heads_t *, const rmm_heads_t *, const void *, const void *, const rmm_rope_t *, const rmm_heads_t *, const rmm_heads_t *, void *, size_t, void *);
+static int (*p_append)(const rmm_heads_t *, const rmm_heads_t *, const rmm_kv4_t *, const void *, const rmm_rope_t *, const rmm_heads_t *, const rmm_heads_t *, void *, size_t, void *);
+static int (*p_read)(const rmm_kv4_t *, const rmm_heads_t *, const rmm_heads_t *, void *, size_t, void *);
+static size_t (*p_kv4_attn_ws)(const rmm_heads_t *, const rmm_kv4_t *);
+static int (*p_kv4_attn)(const rmm_heads_t *, const rmm_kv4_t *, int, double, const rmm_heads_t *, int32_t *, void *, size_t, void *);
 
 /* 1: read; 0: not a plain CUDA tensor of a known dtype (no exception is left set) */
 typedef struct {
@@ -31,6 +36,7 @@ typedef struct {
     PyObject *dtype;   /* borrowed: one of the dtypes above */
     int dims;
     int64_t shape[4], stride[4];
+    long device;       /* set by read_on */
 } tensor_t;
 
 static int read_tensor(PyObject *t, tensor_t *o)
@@ -44,7 +50,7 @@ static int read_tensor(PyObject *t, tensor_t *o)
     if (!ok) return 0;
     ok = 0;
     if ((v = PyObject_GetAttr(t, s_dtype)) == NULL) goto out;
-    o->dtype = v == dt_bf16 ? dt_bf16 : v == dt_f32 ? dt_f32 : NULL;
+    o->dtype = v == dt_bf16 ? dt_bf16 : v == dt_f32 ? dt_f32 : v == dt_i32 ? dt_i32 : v == dt_u8 ? dt_u8 : NULL;
     Py_DECREF(v);
     if (o->dtype == NULL) return 0;
     if ((shape = PyObject_GetAttr(t, s_shape)) == NULL || (stride = PyObject_CallMethodNoArgs(t, s_stride)) == NULL) goto out;
@@ -69,7 +75,7 @@ out:
 static int read_mat(PyObject *t, rmm_mat_t *m, int *dims)
 {
     tensor_t r;
-    if (!read_tensor(t, &r) || (r.dims != 2 && r.dims != 3)) return 0;
+    if (!read_tensor(t, &r) || (r.dims != 2 && r.dims != 3) || (r.dtype != dt_bf16 && r.dtype != dt_f32)) return 0;
     const int b = r.dims - 2;
     m->ptr = r.ptr;
     m->dtype = r.dtype == dt_bf16 ? RMM_BF16 : RMM_F32;
@@ -277,6 +283,240 @@ out:
     return ret;
 }
 
+/* ---- rows of heads and the 4-bit cache.  What is not plain here: a tensor of another device than the current one, and whatever the
+ * Python code would refuse. */
+
+static int current_device(long *index)
+{
+    PyObject *v = PyObject_CallNoArgs(fn_device);
+    if (v == NULL) { PyErr_Clear(); return 0; }
+    *index = PyLong_AsLong(v);
+    Py_DECREF(v);
+    if (PyErr_Occurred()) { PyErr_Clear(); return 0; }
+    return 1;
+}
+
+/* 1: read, and on the given device */
+static int read_on(PyObject *t, tensor_t *o, long device)
+{
+    PyObject *v;
+    if (!read_tensor(t, o)) return 0;
+    if ((v = PyObject_CallMethodNoArgs(t, s_get_device)) == NULL) { PyErr_Clear(); return 0; }
+    o->device = PyLong_AsLong(v);
+    Py_DECREF(v);
+    if (PyErr_Occurred()) { PyErr_Clear(); return 0; }
+    return o->device == device;
+}
+
+static int read_heads(PyObject *t, rmm_heads_t *h, long device)
+{
+    tensor_t r;
+    if (!read_on(t, &r, device) || r.dims != 4 || (r.dtype != dt_bf16 && r.dtype != dt_f32) || (r.stride[3] != 1 && r.shape[3] > 1)) return 0;
+    h->ptr = r.ptr;
+    h->dtype = r.dtype == dt_bf16 ? RMM_BF16 : RMM_F32;
+    h->B = r.shape[0]; h->H = r.shape[1]; h->L = r.shape[2]; h->D = r.shape[3];
+    for (int i = 0; i < 3; ++i) h->stride[i] = r.stride[i];
+    return h->B > 0 && h->H > 0 && h->L > 0 && h->D > 0;
+}
+
+/* A weight [D] (None: NULL); *dtype: -1 before the first, the same for all */
+static int read_weight(PyObject *t, int64_t D, const void **ptr, int *dtype, long device)
+{
+    tensor_t r;
+    *ptr = NULL;
+    if (t == Py_None) return 1;
+    if (!read_on(t, &r, device) || r.dims != 1 || r.shape[0] != D || (r.stride[0] != 1 && D > 1) || (r.dtype != dt_bf16 && r.dtype != dt_f32)) return 0;
+    const int dt = r.dtype == dt_bf16 ? RMM_BF16 : RMM_F32;
+    if (*dtype >= 0 && *dtype != dt) return 0;
+    *dtype = dt;
+    *ptr = r.ptr;
+    return 1;
+}
+
+static int read_rope(PyObject *table, PyObject *eps, PyObject *interleaved, rmm_rope_t *r, long device)
+{
+    tensor_t t;
+    if (!number(eps, &r->eps) || (interleaved != Py_True && interleaved != Py_False)) return 0;
+    r->interleaved = interleaved == Py_True;
+    if (table == Py_None) return 1;
+    if (!read_on(table, &t, device) || t.dims != 2 || t.dtype != dt_f32 || t.stride[1] != 1 || t.shape[0] < 1 || t.shape[1] < 1) return 0;
+    r->table = t.ptr;
+    r->table_rows = t.shape[0];
+    r->rot = t.shape[1];
+    r->table_stride = t.shape[0] > 1 ? t.stride[0] : t.shape[1];
+    return 1;
+}
+
+static int read_ints(PyObject *t, int64_t n, const int32_t **ptr, long device)
+{
+    tensor_t r;
+    if (!read_on(t, &r, device) || r.dims != 1 || r.dtype != dt_i32 || r.shape[0] != n || (r.stride[0] != 1 && n > 1)) return 0;
+    *ptr = r.ptr;
+    return 1;
+}
+
+static int read_cache(PyObject *pool, PyObject *pages, PyObject *lengths, PyObject *new_len, rmm_kv4_t *c, long device)
+{
+    tensor_t p, t;
+    if (!read_on(pool, &p, device) || p.dims != 4 || p.dtype != dt_u8 || p.stride[3] != 1 || p.shape[0] < 1 || p.shape[1] < 1 || p.shape[2] < 1 ||
+        p.shape[3] < 18 || p.shape[3] % 18 != 0 || (p.shape[2] > 1 && p.stride[2] != p.shape[3]))
+        return 0;
+    if (!read_on(pages, &t, device) || t.dims != 2 || t.dtype != dt_i32 || (t.stride[1] != 1 && t.shape[1] > 1)) return 0;
+    c->pool = p.ptr;
+    c->n_pages = p.shape[0]; c->Hkv = p.shape[1]; c->page = 16 * p.shape[2]; c->Dh = p.shape[3] / 18;
+    c->page_stride = c->n_pages > 1 ? p.stride[0] : c->Hkv * p.shape[2] * p.shape[3];
+    c->head_stride = c->Hkv > 1 ? p.stride[1] : p.shape[2] * p.shape[3];
+    c->pages = t.ptr;
+    c->B = t.shape[0]; c->max_pages = t.shape[1]; c->pages_stride = c->B > 1 ? t.stride[0] : c->max_pages;
+    return read_ints(lengths, c->B, &c->lengths, device) && (new_len == Py_None || read_ints(new_len, c->B, &c->new_len, device));
+}
+
+static PyObject *new_heads(PyObject *like, const rmm_heads_t *shape, PyObject *dtype, rmm_heads_t *out)
+{
+    const int64_t size[4] = {shape->B, shape->H, shape->L, shape->D};
+    *out = *shape;
+    out->dtype = dtype == dt_bf16 ? RMM_BF16 : RMM_F32;
+    out->stride[2] = shape->D; out->stride[1] = shape->L * shape->D; out->stride[0] = shape->H * out->stride[1];
+    return new_out(like, 4, size, dtype, &out->ptr);
+}
+
+/* 1: done; 0: an exception is set */
+#define CALL(expression)                                                        \
+    do {                                                                        \
+        Py_BEGIN_ALLOW_THREADS                                                  \
+        rc = (expression);                                                      \
+        if (rc != RMM_OK) { Py_BLOCK_THREADS raise_status(rc); Py_UNBLOCK_THREADS } \
+        Py_END_ALLOW_THREADS                                                    \
+    } while (0)
+
+/* norm_rope(Q, K, q_weight, k_weight, rope, positions, eps, interleaved) -> Q', (Q', K') or None */
+static PyObject *norm_rope(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    rmm_heads_t q, k, qo, ko;
+    rmm_rope_t r = {0};
+    const void *qw, *kw;
+    int dtype = -1, rc;
+    long device;
+    (void)self;
+    if (n != 8 || !current_device(&device) || !read_heads(args[0], &q, device)) Py_RETURN_NONE;
+    const int has_k = args[1] != Py_None;
+    if ((has_k && (!read_heads(args[1], &k, device) || k.dtype != q.dtype)) || !read_weight(args[2], q.D, &qw, &dtype, device) ||
+        !read_weight(args[3], q.D, &kw, &dtype, device) || !read_rope(args[4], args[6], args[7], &r, device))
+        Py_RETURN_NONE;
+    r.weight_dtype = dtype < 0 ? RMM_F32 : dtype;
+    if (args[5] != Py_None) {
+        tensor_t p;
+        if (!read_on(args[5], &p, device) || p.dtype != dt_i32 || (p.dims != 1 && p.dims != 2) || p.shape[p.dims - 1] != q.L) Py_RETURN_NONE;
+        if (p.dims == 2 && p.shape[0] != 1 && p.shape[0] != q.B) Py_RETURN_NONE;
+        r.positions = p.ptr;
+        r.pos_stride[0] = p.dims == 2 && p.shape[0] != 1 ? p.stride[0] : 0;
+        r.pos_stride[1] = p.stride[p.dims - 1];
+    }
+    PyObject *Qo = NULL, *Ko = NULL, *ws = NULL, *ret = NULL, *dt = q.dtype == RMM_BF16 ? dt_bf16 : dt_f32;
+    void *wp, *stream;
+    size_t bytes;
+    if ((Qo = new_heads(args[0], &q, dt, &qo)) == NULL || (has_k && (Ko = new_heads(args[1], &k, dt, &ko)) == NULL)) goto out;
+    if ((ws = workspace_of(args[0], 0, &wp, &bytes)) == NULL || !stream_of(&stream)) goto out;
+    CALL(p_norm_rope(&q, has_k ? &k : NULL, qw, kw, &r, &qo, has_k ? &ko : NULL, wp, bytes, stream));
+    if (rc == RMM_OK) {
+        if (has_k) ret = PyTuple_Pack(2, Qo, Ko);
+        else { ret = Qo; Py_INCREF(ret); }
+    }
+out:
+    Py_XDECREF(Qo);
+    Py_XDECREF(Ko);
+    Py_XDECREF(ws);
+    return ret;
+}
+
+/* kv4_append(K, V, pool, pages, lengths, new_len, k_weight, rope, eps, interleaved, want_values) -> (K', V'), False (done, nothing asked for) or None */
+static PyObject *kv4_append(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    rmm_heads_t k, v, ko, vo;
+    rmm_rope_t r = {0};
+    rmm_kv4_t c = {0};
+    const void *kw;
+    int dtype = -1, rc;
+    long device;
+    (void)self;
+    if (n != 11 || !current_device(&device) || !read_heads(args[0], &k, device) || !read_heads(args[1], &v, device) ||
+        !read_cache(args[2], args[3], args[4], args[5], &c, device) || !read_weight(args[6], k.D, &kw, &dtype, device) ||
+        !read_rope(args[7], args[8], args[9], &r, device) || (args[10] != Py_True && args[10] != Py_False))
+        Py_RETURN_NONE;
+    r.weight_dtype = dtype < 0 ? RMM_F32 : dtype;
+    const int held = args[10] == Py_True;
+    PyObject *Ko = NULL, *Vo = NULL, *ws = NULL, *ret = NULL;
+    void *wp, *stream;
+    size_t bytes;
+    if (held && ((Ko = new_heads(args[0], &k, dt_bf16, &ko)) == NULL || (Vo = new_heads(args[0], &k, dt_bf16, &vo)) == NULL)) goto out;
+    if ((ws = workspace_of(args[0], 0, &wp, &bytes)) == NULL || !stream_of(&stream)) goto out;
+    CALL(p_append(&k, &v, &c, kw, &r, held ? &ko : NULL, held ? &vo : NULL, wp, bytes, stream));
+    if (rc == RMM_OK) {
+        if (held) ret = PyTuple_Pack(2, Ko, Vo);
+        else { ret = Py_False; Py_INCREF(ret); }
+    }
+out:
+    Py_XDECREF(Ko);
+    Py_XDECREF(Vo);
+    Py_XDECREF(ws);
+    return ret;
+}
+
+/* kv4_read(pool, pages, lengths, new_len, rows, dtype) -> (K, V) or None */
+static PyObject *kv4_read(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    rmm_kv4_t c = {0};
+    rmm_heads_t shape = {0}, k, v;
+    int rc;
+    long device;
+    (void)self;
+    if (n != 6 || !current_device(&device) || !read_cache(args[0], args[1], args[2], args[3], &c, device) || !PyLong_CheckExact(args[4]) ||
+        (args[5] != dt_bf16 && args[5] != dt_f32))
+        Py_RETURN_NONE;
+    shape.B = c.B; shape.H = c.Hkv; shape.L = PyLong_AsLongLong(args[4]); shape.D = c.Dh;
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    if (shape.B < 1 || shape.L < 1) Py_RETURN_NONE;
+    PyObject *K = NULL, *V = NULL, *ws = NULL, *ret = NULL;
+    void *wp, *stream;
+    size_t bytes;
+    if ((K = new_heads(args[0], &shape, args[5], &k)) == NULL || (V = new_heads(args[0], &shape, args[5], &v)) == NULL) goto out;
+    if ((ws = workspace_of(args[0], 0, &wp, &bytes)) == NULL || !stream_of(&stream)) goto out;
+    CALL(p_read(&c, &k, &v, wp, bytes, stream));
+    if (rc == RMM_OK) ret = PyTuple_Pack(2, K, V);
+out:
+    Py_XDECREF(K);
+    Py_XDECREF(V);
+    Py_XDECREF(ws);
+    return ret;
+}
+
+/* kv4_attn(Q, pool, pages, lengths, new_len, causal, rho_d) -> O or None */
+static PyObject *kv4_attn(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    rmm_kv4_t c = {0};
+    rmm_heads_t q, o;
+    double rho_d;
+    int rc;
+    long device;
+    (void)self;
+    if (n != 7 || !current_device(&device) || !read_heads(args[0], &q, device) || !read_cache(args[1], args[2], args[3], args[4], &c, device) ||
+        (args[5] != Py_True && args[5] != Py_False) || !number(args[6], &rho_d))
+        Py_RETURN_NONE;
+    const size_t need = p_kv4_attn_ws(&q, &c);
+    if (need == 0) Py_RETURN_NONE;
+    PyObject *O = NULL, *ws = NULL, *ret = NULL;
+    void *wp, *stream;
+    size_t bytes;
+    if ((O = new_heads(args[0], &q, dt_bf16, &o)) == NULL) goto out;
+    if ((ws = workspace_of(args[0], need, &wp, &bytes)) == NULL || !stream_of(&stream)) goto out;
+    CALL(p_kv4_attn(&q, &c, args[5] == Py_True, rho_d, &o, NULL, wp, bytes, stream));
+    if (rc == RMM_OK) { ret = O; Py_INCREF(ret); }
+out:
+    Py_XDECREF(O);
+    Py_XDECREF(ws);
+    return ret;
+}
+
 static PyObject *set_poison(PyObject *self, PyObject *on)
 {
     (void)self;
@@ -284,13 +524,13 @@ static PyObject *set_poison(PyObject *self, PyObject *on)
     Py_RETURN_NONE;
 }
 
-/* init(library path, (Tensor, Parameter), (bfloat16, float32, int32), (raw stream, current device), the module's names) */
+/* init(library path, (Tensor, Parameter), (bfloat16, float32, int32, uint8), (raw stream, current device), the module's names) */
 static PyObject *init(PyObject *self, PyObject *args)
 {
     const char *path;
     PyObject *tt, *tp;
     (void)self;
-    if (!PyArg_ParseTuple(args, "s(OO)(OOO)(OO)O!", &path, &tt, &tp, &dt_bf16, &dt_f32, &dt_i32, &fn_stream, &fn_device, &PyDict_Type,
+    if (!PyArg_ParseTuple(args, "s(OO)(OOOO)(OO)O!", &path, &tt, &tp, &dt_bf16, &dt_f32, &dt_i32, &dt_u8, &fn_stream, &fn_device, &PyDict_Type,
                           &names))
         return NULL;
     void *h = dlopen(path, RTLD_NOW);
@@ -302,13 +542,19 @@ static PyObject *init(PyObject *self, PyObject *args)
     *(void **)&p_product = dlsym(h, "rmm_product");
     *(void **)&p_attn_ws = dlsym(h, "rmm_reduced_attn_workspace_bytes");
     *(void **)&p_attn = dlsym(h, "rmm_reduced_attn");
-    if (!p_keep_count || !p_product_ws || !p_score_ws || !p_gemm_ws || !p_product || !p_attn_ws || !p_attn) {
+    *(void **)&p_norm_rope = dlsym(h, "rmm_qk_norm_rope");
+    *(void **)&p_append = dlsym(h, "rmm_kv4_append");
+    *(void **)&p_read = dlsym(h, "rmm_kv4_read");
+    *(void **)&p_kv4_attn_ws = dlsym(h, "rmm_kv4_attn_workspace_bytes");
+    *(void **)&p_kv4_attn = dlsym(h, "rmm_kv4_attn");
+    if (!p_keep_count || !p_product_ws || !p_score_ws || !p_gemm_ws || !p_product || !p_attn_ws || !p_attn || !p_norm_rope || !p_append || !p_read ||
+        !p_kv4_attn_ws || !p_kv4_attn) {
         PyErr_SetString(PyExc_RuntimeError, "librmm_b200.so lacks an entry point");
         return NULL;
     }
     type_tensor = (PyTypeObject *)tt;
     type_parameter = (PyTypeObject *)tp;
-    PyObject *keep[] = {tt, tp, dt_bf16, dt_f32, dt_i32, fn_stream, fn_device, names};
+    PyObject *keep[] = {tt, tp, dt_bf16, dt_f32, dt_i32, dt_u8, fn_stream, fn_device, names};
     for (size_t i = 0; i < sizeof keep / sizeof *keep; ++i) Py_INCREF(keep[i]);   /* for the life of the process */
     Py_RETURN_NONE;
 }
@@ -318,6 +564,10 @@ static PyMethodDef methods[] = {
     {"set_poison", set_poison, METH_O, NULL},
     {"product", (PyCFunction)(void (*)(void))product, METH_FASTCALL, NULL},
     {"attn", (PyCFunction)(void (*)(void))attn, METH_FASTCALL, NULL},
+    {"norm_rope", (PyCFunction)(void (*)(void))norm_rope, METH_FASTCALL, NULL},
+    {"kv4_append", (PyCFunction)(void (*)(void))kv4_append, METH_FASTCALL, NULL},
+    {"kv4_read", (PyCFunction)(void (*)(void))kv4_read, METH_FASTCALL, NULL},
+    {"kv4_attn", (PyCFunction)(void (*)(void))kv4_attn, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "rmm_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
