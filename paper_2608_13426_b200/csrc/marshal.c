@@ -39,6 +39,8 @@ typedef struct {
     long device;       /* set by read_on */
 } tensor_t;
 
+static void find_exchange(PyObject *tensor_type);
+
 static int read_tensor(PyObject *t, tensor_t *o)
 {
     PyObject *v, *shape = NULL, *stride = NULL;
@@ -296,10 +298,56 @@ static int current_device(long *index)
     return 1;
 }
 
+/* The tensors' exchange table of the DLPack protocol (its published C structures): a description of a tensor in one C call.
+ * NULL where this torch has none: the attributes are then read one by one. */
+typedef struct { int32_t type, id; } dl_device;
+typedef struct { uint8_t code, bits; uint16_t lanes; } dl_dtype;
+typedef struct { void *data; dl_device device; int32_t ndim; dl_dtype dtype; int64_t *shape, *strides; uint64_t byte_offset; } dl_tensor;
+typedef struct dl_header { struct { uint32_t major, minor; } version; struct dl_header *prev; } dl_header;
+typedef struct {
+    dl_header header;
+    void *managed_tensor_allocator, *managed_tensor_from_py_object, *managed_tensor_to_py_object;
+    int (*dltensor_from_py_object)(void *, dl_tensor *);
+    void *current_work_stream;
+} dl_exchange;
+enum { DL_CUDA = 2, DL_INT = 0, DL_UINT = 1, DL_FLOAT = 2, DL_BFLOAT = 4, DL_MAJOR = 1 };
+static const dl_exchange *exchange;
+
+static void find_exchange(PyObject *tensor_type)
+{
+    PyObject *capsule = PyObject_GetAttrString(tensor_type, "__dlpack_c_exchange_api__");
+    if (capsule != NULL && PyCapsule_CheckExact(capsule)) {
+        const dl_exchange *e = PyCapsule_GetPointer(capsule, "dlpack_exchange_api");
+        if (e != NULL && e->header.version.major == DL_MAJOR && e->dltensor_from_py_object != NULL) exchange = e;
+    }
+    Py_XDECREF(capsule);   /* (the table lives as long as the process) */
+    PyErr_Clear();
+}
+
 /* 1: read, and on the given device */
 static int read_on(PyObject *t, tensor_t *o, long device)
 {
     PyObject *v;
+    if (exchange != NULL) {
+        dl_tensor d;
+        if (Py_TYPE(t) != type_tensor && Py_TYPE(t) != type_parameter) return 0;
+        if (exchange->dltensor_from_py_object(t, &d) != 0) { PyErr_Clear(); return 0; }
+        if (d.device.type != DL_CUDA || d.device.id != device || d.ndim < 1 || d.ndim > 4 || d.dtype.lanes != 1 || d.strides == NULL) return 0;
+        o->dtype = d.dtype.code == DL_BFLOAT && d.dtype.bits == 16  ? dt_bf16
+                   : d.dtype.code == DL_FLOAT && d.dtype.bits == 32 ? dt_f32
+                   : d.dtype.code == DL_INT && d.dtype.bits == 32   ? dt_i32
+                   : d.dtype.code == DL_UINT && d.dtype.bits == 8   ? dt_u8
+                                                                    : NULL;
+        if (o->dtype == NULL) return 0;
+        o->ptr = (char *)d.data + d.byte_offset;
+        o->dims = d.ndim;
+        for (int i = 0; i < d.ndim; ++i) {
+            o->shape[i] = d.shape[i];
+            o->stride[i] = d.strides[i];
+        }
+        o->device = device;
+        return 1;
+    }
     if (!read_tensor(t, o)) return 0;
     if ((v = PyObject_CallMethodNoArgs(t, s_get_device)) == NULL) { PyErr_Clear(); return 0; }
     o->device = PyLong_AsLong(v);
@@ -552,6 +600,7 @@ static PyObject *init(PyObject *self, PyObject *args)
         PyErr_SetString(PyExc_RuntimeError, "librmm_b200.so lacks an entry point");
         return NULL;
     }
+    find_exchange(tt);
     type_tensor = (PyTypeObject *)tt;
     type_parameter = (PyTypeObject *)tp;
     PyObject *keep[] = {tt, tp, dt_bf16, dt_f32, dt_i32, dt_u8, fn_stream, fn_device, names};
