@@ -2,7 +2,7 @@
 //
 // Values: 64 columns of one token and head share a step s and a least value m, both bf16:  x = m + s n,  n = 0 .. 15,
 //   m = min x,  s = bf16((max x - m) / 15),  n = min(15, round((x - m) / s))  (0 where s = 0; halves to the even code),
-// taken on bf16 numbers, so m is exact; x - m is taken in fp32, the quotient is exact.  4.5 bits a value.
+// taken on bf16 numbers, so m is exact; difference and quotient are fp32's.  4.5 bits a value.
 //
 // Layout: 16 tokens of one kv head are one block of 18 Dh contiguous bytes, so one bulk copy brings keys, values and steps of a
 // block.  The codes lie in the order in which the attention's matrix instructions want them, eight columns to a 32-bit word:

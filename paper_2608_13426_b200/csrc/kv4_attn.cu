@@ -34,6 +34,7 @@ namespace {
 
 constexpr int kWarps = 4, kPair = 2 * kv4::kBlock;   // warps of a CTA; tokens of a warp's turn
 constexpr int kFixed = 12, kLeast = kFixed + 8;      // pairs that a job's fixed part counts as; the least share of a CTA
+constexpr int kCut = 1;                              // a job of that many shares is cut into pieces of its own
 constexpr float kTopWeight = 16384.f, kTop = 6.f, kLeastStep = 8.2718061e-25f;   // 2^14, log2 of 2^6, 2^-80: see above; smaller steps weigh as that
 constexpr float kNone = 1e30f;                       // minus the reference of a row that has seen no key
 
@@ -46,7 +47,8 @@ struct AttnArgs {
     int causal;
     float scale_log2;
     const uint32_t *kept;     // [B][Hq][D / 32] bit masks of the kept features, or NULL: all
-    float *part;              // [2 CTAs][rows][D + 2]: sums, then (reference, sum of weights)
+    float *part;              // [2 CTAs][rows][D + 4]: sums in the order of the merge, then reference and sum of weights
+    int q_vec, o_pairs;       // rows of Q on 16-byte boundaries, of O on 4-byte ones
     unsigned *counters;
     int *status;
     unsigned long long wait_ns;
@@ -58,13 +60,14 @@ struct Shape {
     static constexpr int kRows = 8 * NT, kBlockBytes = 18 * D, kPairBytes = 2 * kBlockBytes, kGroups = D / 64;
     static constexpr int kCtas = D * NT <= 128 ? 4 : 2;                        // an SM
     static constexpr int kStages = D == 64 ? (NT == 1 ? 4 : 3) : (D == 128 && NT == 2 ? 4 : 2);
-    static constexpr int kPitchM = 66;
+    static constexpr int kPitchM = 68, kPitchP = D + 4;                        // of a row in the merge and among the parts
     static constexpr int kOffQ = kWarps * kStages * kPairBytes;                // fp16 fragments [row tile of 8][D / 32][lane][4 words]
     static constexpr int kOffMerge = kOffQ + kRows * D * 2;                    // fp32 [warp][row][pitch]
-    static constexpr int kOffMl = kOffMerge + kWarps * kRows * kPitchM * 4;    // [warp][row]: (reference, sum), then the warp's factor
+    static constexpr int kOffOut = kOffMerge + kWarps * kRows * kPitchM * 4;   // [row]: where its output lies (elements), or -1
+    static constexpr int kOffMl = kOffOut + kRows * 8;                         // [warp][row]: (reference, sum), then the warp's factor
     static constexpr int kOffRow = kOffMl + kWarps * kRows * 8;                // [row]: scale, visible keys, then sums of q by group
-    static constexpr int kOffTot = kOffRow + kRows * (2 + kGroups) * 4;        // [row]: reference, sum of the CTA
-    static constexpr int kOffBar = (kOffTot + kRows * 8 + 15) / 16 * 16;       // barriers, then the tokens of each ring entry
+    static constexpr int kOffTot = kOffRow + kRows * (2 + kGroups) * 4;        // [row]: reference and sum of the CTA, one over the sum
+    static constexpr int kOffBar = (kOffTot + kRows * 12 + 15) / 16 * 16;      // barriers, then the tokens of each ring entry
     static constexpr int kSmem = kOffBar + kWarps * kStages * 12;
     static_assert((kSmem + 1280) * kCtas <= 227 * 1024, "shared memory");   // (1 KB a CTA is the system's)
 };
@@ -116,7 +119,7 @@ __device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c, int shar
     kv4::sequence(a.cache, c.b, c.len, c.rows, a.status);
     c.nb = (c.len + kPair - 1) / kPair;
     c.valid = (c.rows * a.group + ROWS - 1) / ROWS;
-    c.each = c.len == 0 ? 1 : (c.nb + kFixed >= share ? 0 : c.nb + kFixed);
+    c.each = c.len == 0 ? 1 : ((c.nb + kFixed) / kCut >= share ? 0 : c.nb + kFixed);
 }
 __device__ __forceinline__ int head_cost(const AttnArgs &a, const Job &c) { return c.valid * c.each + a.chunks - c.valid; }
 __device__ __forceinline__ int pieces_of(const Job &c, int share)   // of a reading job that is cut
@@ -201,6 +204,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32, THREADS = kWarps * 32;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int s_scan[2][kWarps], s_begin[2], s_pending[2][5], abort_flag, s_last[2];
+    int64_t *row_out = reinterpret_cast<int64_t *>(smem + S::kOffOut);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * ST * S::kPairBytes, bars = smem_u32(smem) + S::kOffBar + warp * ST * 8;
     int *tokens = reinterpret_cast<int *>(smem + S::kOffBar + kWarps * ST * 8) + warp * ST;   // of the first block, + 256 x of the second
@@ -217,18 +221,50 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     pdl_wait();
 
     // ---- this CTA's share
-    auto scan = [&](int (&v)[2], int (&sum)[2]) {   // inclusive, over the block
+    Job cur;
+    int total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+        int v = 0;
+        cur.b = b0 + tid;
+        if (cur.b < a.B) {
+            job_sequence<ROWS>(a, cur, INT32_MAX);
+            v = a.Hkv * head_cost(a, cur);
+        }
+        v = __reduce_add_sync(0xffffffffu, v);
+        if (b0 > 0) __syncthreads();
+        if (lane == 0) s_scan[0][warp] = v;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) total += s_scan[0][w];
+    }
+    const int share = max(kLeast, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+    // CTAs with a piece of a job, and what the other jobs count: this thread's sequence, the sequences up to it, all
+    int mine[2] = {0, 0}, upto[2] = {0, 0}, sum[2] = {0, 0};
+    auto scan = [&](int b0) {
+        if (a.B > THREADS) {
+            cur.b = b0 + tid;
+            if (cur.b < a.B) job_sequence<ROWS>(a, cur, share);
+        } else if (cur.b < a.B && cur.len > 0 && cur.each >= share) {
+            cur.each = 0;
+        }
+        mine[0] = mine[1] = 0;
+        if (cur.b < a.B) {
+            mine[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, share) : 0;
+            mine[1] = a.Hkv * head_cost(a, cur);
+        }
+        upto[0] = mine[0];
+        upto[1] = mine[1];
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int o = __shfl_up_sync(0xffffffffu, v[i], d);
-                if (lane >= d) v[i] += o;
+                const int o = __shfl_up_sync(0xffffffffu, upto[i], d);
+                if (lane >= d) upto[i] += o;
             }
         __syncthreads();
         if (lane == 31) {
-            s_scan[0][warp] = v[0];
-            s_scan[1][warp] = v[1];
+            s_scan[0][warp] = upto[0];
+            s_scan[1][warp] = upto[1];
         }
         __syncthreads();
 #pragma unroll
@@ -236,58 +272,26 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             sum[i] = 0;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                if (w == warp) v[i] += sum[i];
+                if (w == warp) upto[i] += sum[i];
                 sum[i] += s_scan[i][w];
             }
         }
     };
-    Job cur;
-    int total = 0;
+    int n_pieces = 0, axis = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-        int v[2] = {0, 0}, sum[2];
-        cur.b = b0 + tid;
-        if (cur.b < a.B) {
-            job_sequence<ROWS>(a, cur, INT32_MAX);
-            v[0] = a.Hkv * head_cost(a, cur);
-        }
-        scan(v, sum);
-        total += sum[0];
-    }
-    const int share = max(kLeast, (total + (int)gridDim.x - 1) / (int)gridDim.x);
-    int n_pieces = 0, axis = 0, mine[2] = {0, 0}, upto[2] = {0, 0};   // CTAs with a piece of a job; what the other jobs count
-    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-        int sum[2];
-        upto[0] = upto[1] = 0;
-        if (a.B > THREADS) cur.b = b0 + tid;
-        if (cur.b < a.B) {
-            job_sequence<ROWS>(a, cur, share);
-            upto[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, share) : 0;
-            upto[1] = a.Hkv * head_cost(a, cur);
-        }
-        mine[0] = upto[0];
-        mine[1] = upto[1];
-        scan(upto, sum);
+        scan(b0);
         n_pieces += sum[0];
         axis += sum[1];
     }
     const bool piece = (int)blockIdx.x < n_pieces;
     const int ctas = min((int)gridDim.x - n_pieces, (axis + kLeast - 1) / kLeast), cta = (int)blockIdx.x - n_pieces;   // of the axis
     if (cta >= ctas) return;
-    int u_begin = piece ? (int)blockIdx.x : (int)((int64_t)axis * cta / ctas), u_end = piece ? 0 : (int)((int64_t)axis * (cta + 1) / ctas);
+    // equal shares: the first `rest` CTAs of the axis have `each` + 1, the others `each`
+    const int each = ctas > 0 ? axis / ctas : 0, rest = axis - each * ctas;
+    auto owner = [&](int at) { return at < rest * (each + 1) ? at / (each + 1) : rest + (at - rest * (each + 1)) / each; };
+    int u_begin = piece ? (int)blockIdx.x : each * cta + min(cta, rest), u_end = piece ? 0 : u_begin + each + (cta < rest ? 1 : 0);
     for (int b0 = 0, base = 0; b0 < a.B; b0 += THREADS) {
-        int sum[2] = {0, 0};
-        if (a.B > THREADS) {
-            cur.b = b0 + tid;
-            upto[0] = upto[1] = 0;
-            if (cur.b < a.B) {
-                job_sequence<ROWS>(a, cur, share);
-                upto[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, share) : 0;
-                upto[1] = a.Hkv * head_cost(a, cur);
-            }
-            mine[0] = upto[0];
-            mine[1] = upto[1];
-            scan(upto, sum);
-        }
+        if (a.B > THREADS) scan(b0);
         const int i = piece ? 0 : 1;
         if (u_begin >= base + upto[i] - mine[i] && u_begin < base + upto[i]) {
             s_begin[0] = b0 + tid;
@@ -302,14 +306,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     job_sequence<ROWS>(a, cur, share);
     if (piece) {
         pieces = pieces_of(cur, share);
-        const int off = u_begin - s_begin[1], job = off / pieces, k = off - job * pieces;
+        const int off = u_begin - s_begin[1], job = off / pieces, k = off - job * pieces, nb = cur.nb / pieces, more = cur.nb - nb * pieces;
         piece0 = (int)blockIdx.x - k;
         cur.hk = job / cur.valid;
         cur.chunk = job - cur.hk * cur.valid;
         cur.each = cur.nb + kFixed;   // alone on an axis of its own
         start = 0;
-        u_begin = kFixed + (int)((int64_t)cur.nb * k / pieces);
-        u_end = kFixed + (int)((int64_t)cur.nb * (k + 1) / pieces);
+        u_begin = kFixed + nb * k + min(k, more);
+        u_end = u_begin + nb + (k < more ? 1 : 0);
     } else {
         const int per_head = head_cost(a, cur);
         int off = u_begin - s_begin[1];
@@ -323,25 +327,23 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     auto first_pair = [&](int at) { return max(0, u_begin - at - kFixed); };
     auto last_pair = [&](const Job &c, int at) { return min(c.nb, u_end - at - kFixed); };
 
-    // ---- Q of a row tile: row i * group + h of the kv head's rows (asked for before the keys are, whose page numbers come first)
-    constexpr int QR = ROWS / kWarps;   // rows of a warp
-    float qx[QR][W32];
+    // ---- Q of a row tile: row i * group + h of the kv head's rows (asked for before the keys are, whose page numbers come first).
+    // D / 8 lanes share a row, eight columns each.
+    constexpr int QL = D / 8, QT = (ROWS * QL + THREADS - 1) / THREADS;   // rows that a lane takes part in
+    Raw8<__nv_bfloat16> q_raw[QT];
+    uint32_t q_kept[QT];
+    auto q_row = [&](int k) { return (k * THREADS + tid) / QL; };
     auto load_q = [&]() {
-        const int row0 = cur.chunk * ROWS, nrows = min(ROWS, cur.rows * a.group - row0);
+        const int row0 = cur.chunk * ROWS, nrows = min(ROWS, cur.rows * a.group - row0), c = tid % QL;
 #pragma unroll
-        for (int k = 0; k < QR; ++k) {
-            const int r = k * kWarps + warp, i = (row0 + r) / a.group, h = (row0 + r) - i * a.group;
-            const int64_t head = (int64_t)cur.hk * a.group + h;
-#pragma unroll
-            for (int v = 0; v < W32; ++v) qx[k][v] = 0.f;
+        for (int k = 0; k < QT; ++k) {
+            const int r = q_row(k), i = (row0 + r) / a.group;
+            q_raw[k] = zero_raw<__nv_bfloat16>();
+            q_kept[k] = 0xffu;
             if (r < nrows) {
-                const __nv_bfloat16 *qp = a.q + cur.b * a.q_sb + head * a.q_sh + (int64_t)i * a.q_sr + lane;
-                const uint32_t *kp = a.kept + ((int64_t)cur.b * a.Hkv * a.group + head) * W32;
-#pragma unroll
-                for (int v = 0; v < W32; ++v) qx[k][v] = __bfloat162float(qp[v * 32]);
-                if (a.kept != nullptr)
-#pragma unroll
-                    for (int v = 0; v < W32; ++v) qx[k][v] = kp[v] >> lane & 1u ? qx[k][v] : 0.f;
+                const int64_t head = (int64_t)cur.hk * a.group + row0 + r - i * a.group;
+                q_raw[k] = load_raw(a.q + cur.b * a.q_sb + head * a.q_sh + (int64_t)i * a.q_sr + 8 * c, a.q_vec != 0);
+                if (a.kept != nullptr) q_kept[k] = a.kept[((int64_t)cur.b * a.Hkv * a.group + head) * W32 + c / 4] >> (8 * (c % 4));
             }
         }
     };
@@ -387,9 +389,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     };
     auto request = [&]() {
         if (p_t >= p_end) return;
-        const int n = __shfl_sync(0xffffffffu, p_tokens, p_k);
-        const uint64_t src0 = __shfl_sync(0xffffffffu, from0, p_k), src1 = split ? __shfl_sync(0xffffffffu, from1, p_k) : 0;
-        if (lane == 0) {
+        if (lane == p_k) {   // the lane that knows the pair
+            const int n = p_tokens;
+            const uint64_t src0 = from0, src1 = from1;
             const uint32_t bar = bars + 8 * p_slot, dst = ring + (uint32_t)p_slot * S::kPairBytes;
             const uint32_t b0 = n & 255 ? S::kBlockBytes : 0, b1 = n >> 8 ? S::kBlockBytes : 0;
             auto copy = [&](uint32_t to, uint64_t from, uint32_t bytes) {
@@ -419,6 +421,20 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     settle();
     for (int i = 0; i < ST; ++i) request();
 
+    // columns 64 j + 8 (2 (c % 4)) + 2 (c / 4), the next, and those 8 on, of an output row
+    auto put = [&](int64_t row, int j, int c, float4 v, float inv) {
+        if (row < 0) return;
+        __nv_bfloat16 *o = a.o + row + 64 * j + 16 * (c & 3) + 2 * (c >> 2);
+        const uint32_t lo = pack_bf16(v.x * inv, v.y * inv), hi = pack_bf16(v.z * inv, v.w * inv);
+        if (a.o_pairs) {
+            *reinterpret_cast<uint32_t *>(o) = lo;
+            *reinterpret_cast<uint32_t *>(o + 8) = hi;
+        } else {
+            unsigned short *h = reinterpret_cast<unsigned short *>(o);
+            h[0] = (unsigned short)lo; h[1] = (unsigned short)(lo >> 16); h[8] = (unsigned short)hi; h[9] = (unsigned short)(hi >> 16);
+        }
+    };
+
     int slot = 0;
     uint32_t phases = 0;
     bool dead = false, first = true;
@@ -433,31 +449,35 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             // ---- Q scaled to fp16
             if (!first) load_q();
 #pragma unroll
-            for (int k = 0; k < QR; ++k) {
-                const int r = k * kWarps + warp, i = (row0 + r) / a.group;
-                const float (&x)[W32] = qx[k];
-                float top = 0.f;
+            for (int k = 0; k < QT; ++k) {
+                const int r = q_row(k), c = tid % QL;
+                if (QT * THREADS > ROWS * QL && r >= ROWS) break;
+                float x[8], top = 0.f, sum = 0.f;
 #pragma unroll
-                for (int v = 0; v < W32; ++v) top = fmaxf(top, fabsf(x[v]));
-                top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t w = q_raw[k].w[e / 2];
+                    x[e] = q_kept[k] >> e & 1u ? (e & 1 ? __uint_as_float(w & 0xffff0000u) : bf16_bits(w)) : 0.f;
+                    top = fmaxf(top, fabsf(x[e]));
+                    sum += x[e];
+                }
+                constexpr uint32_t lanes = 0xffffffffu;
+#pragma unroll
+                for (int d = QL / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(lanes, top, d));
+#pragma unroll
+                for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(lanes, sum, d);   // of 64 columns
                 // 2^e at top; a row of zeros, or one too small or large to scale, is taken as it is
                 const int e = (int)(__float_as_uint(top) >> 23) - 127;
                 const int shift = e < -100 || e > 100 ? 0 : 14 - e;
-                const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-                // Column 8 t + c of 32: lane 4 (r % 8) + t, words (c = 0, 4) (1, 5) (2, 6) (3, 7).  Odd columns meet codes four bits up.
-                const int c = lane & 7, at = ((r & 7) * 4 + (lane >> 3)) * 8 + (c & 3) * 2 + (c >> 2);
-#pragma unroll
-                for (int v = 0; v < W32; ++v) qs[((r >> 3) * W32 + v) * 256 + at] = __float2half_rn(x[v] * up * (lane & 1 ? 0.0625f : 1.f));
-#pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    float sum = x[2 * j] + x[2 * j + 1];
-#pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                    if (lane == 0) row_sum[r * NG + j] = sum * __uint_as_float((uint32_t)(127 + shift - 24) << 23);
-                }
-                if (lane == 0) {
+                const float up = __uint_as_float((uint32_t)(127 + shift) << 23), up4 = 0.0625f * up;   // odd columns meet codes four bits up
+                // columns 8 t .. of 32: lane 4 (r % 8) + t, words (c = 0, 4) (1, 5) (2, 6) (3, 7)
+                reinterpret_cast<uint4 *>(qs)[((r >> 3) * W32 + c / 4) * 32 + (r & 7) * 4 + c % 4] =
+                    make_uint4(pack_f16(x[0] * up, x[4] * up), pack_f16(x[1] * up4, x[5] * up4), pack_f16(x[2] * up, x[6] * up), pack_f16(x[3] * up4, x[7] * up4));
+                if (c % 8 == 0) row_sum[r * NG + c / 8] = sum * __uint_as_float((uint32_t)(127 + shift - 24) << 23);
+                if (c == 0) {
+                    const int row = row0 + r, i = row / a.group;
                     row_scale[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - shift + 24) << 23);
                     row_vis[r] = r < nrows ? (a.causal ? max(0, min(cur.len, cur.len - cur.rows + i + 1)) : cur.len) : 0;
+                    row_out[r] = i < a.L ? cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - i * a.group) * a.o_sh + (int64_t)i * a.o_sr : -1;
                 }
             }
             __syncthreads();
@@ -708,10 +728,12 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     sum = fmaf(f, ml[(w * ROWS + tid) * 2 + 1], sum);
                     ml[(w * ROWS + tid) * 2] = f;
                 }
-                tot[tid * 2] = mx;
-                tot[tid * 2 + 1] = tid < nrows ? sum : 0.f;   // (rows that are none have met keys all the same)
+                sum = tid < nrows ? sum : 0.f;   // (rows that are none have met keys all the same)
+                tot[tid * 3] = mx;
+                tot[tid * 3 + 1] = sum;
+                tot[tid * 3 + 2] = sum == 0.f ? 0.f : 1.f / sum;   // (0: the row sees no key; a NaN stays one)
             }
-            float *part = whole ? nullptr : a.part + (int64_t)(2 * blockIdx.x + (t0 == 0 ? 1 : 0)) * ROWS * (D + 2);
+            float *part = a.part + (int64_t)(2 * blockIdx.x + (t0 == 0 ? 1 : 0)) * ROWS * S::kPitchP;
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
                 if (j > 0) __syncthreads();
@@ -719,28 +741,28 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float *dst = merge + (warp * ROWS + nt * 8 + 2 * t4 + e) * S::kPitchM + 8 * g;
+                        float *dst = merge + (warp * ROWS + nt * 8 + 2 * t4 + e) * S::kPitchM + 2 * g;
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)   // columns 8 g + 2 q and the next, whose codes lay four bits up
-                            *reinterpret_cast<float2 *>(dst + 2 * q) = make_float2(fmaf(o[nt][j * 4 + q][e], 16777216.f, low[nt][e][j]),
-                                                                                   fmaf(o[nt][j * 4 + q][e + 2], 1048576.f, low[nt][e][j]));
+                        for (int q = 0; q < 4; ++q)   // columns 8 g + 2 q and the next, whose codes lay four bits up, at 16 q + 2 g
+                            *reinterpret_cast<float2 *>(dst + 16 * q) = make_float2(fmaf(o[nt][j * 4 + q][e], 16777216.f, low[nt][e][j]),
+                                                                                    fmaf(o[nt][j * 4 + q][e + 2], 1048576.f, low[nt][e][j]));
                     }
                 __syncthreads();
-#pragma unroll 4
-                for (int i = tid; i < ROWS * 64; i += THREADS) {
-                    const int r = i >> 6, c = i & 63;
-                    float sum = 0.f;
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) sum = fmaf(ml[(w * ROWS + r) * 2], merge[(w * ROWS + r) * S::kPitchM + c], sum);
-                    const float lsum = tot[r * 2 + 1];
+                for (int k = 0; k < NT; ++k) {
+                    const int r = k * 8 + (tid >> 4), c = tid & 15;
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        const float f = ml[(w * ROWS + r) * 2];
+                        const float4 v = *reinterpret_cast<const float4 *>(merge + (w * ROWS + r) * S::kPitchM + 4 * c);
+                        sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+                    }
                     if (whole) {
-                        const int row = row0 + r, qi = row / a.group;
-                        if (qi < a.L)
-                            a.o[cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr + j * 64 + c] =
-                                __float2bfloat16_rn(lsum == 0.f ? 0.f : sum * (1.f / lsum));   // (0: the row sees no key; a NaN stays one)
+                        put(row_out[r], j, c, sum, tot[r * 3 + 2]);
                     } else {
-                        part[r * (D + 2) + j * 64 + c] = sum;
-                        if (j == 0 && c < 2) part[r * (D + 2) + D + c] = tot[r * 2 + c];
+                        *reinterpret_cast<float4 *>(part + r * S::kPitchP + j * 64 + 4 * c) = sum;
+                        if (j == 0 && c == 0) *reinterpret_cast<float2 *>(part + r * S::kPitchP + D) = make_float2(tot[r * 3], tot[r * 3 + 1]);
                     }
                 }
             }
@@ -749,9 +771,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             if (!whole && tid == 0) {   // other CTAs work on this job too: the first and last of them are
                 int c0 = piece0, c1 = piece0 + pieces - 1;
                 if (!piece) {
-                    const int64_t job0 = start + kFixed, job1 = job0 + cur.nb - 1;   // its first and last pair on the axis
-                    c0 = n_pieces + (int)(((job0 + 1) * ctas - 1) / axis);
-                    c1 = n_pieces + (int)(((job1 + 1) * ctas - 1) / axis);
+                    c0 = n_pieces + owner(start + kFixed);   // of its first and last pair
+                    c1 = n_pieces + owner(start + kFixed + cur.nb - 1);
                 }
                 int *to = s_pending[t0 == 0 ? 1 : 0];
                 to[0] = c0;
@@ -783,29 +804,33 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         if (!s_last[k]) continue;
         const int c0 = s_pending[k][0], c1 = s_pending[k][1], row0 = s_pending[k][4];
         const int64_t b = s_pending[k][2], hk = s_pending[k][3];
-        for (int r = warp; r < ROWS; r += kWarps) {
-            const int row = row0 + r, qi = row / a.group;
-            if (qi >= a.L) continue;
-            const float *src = a.part + r * (D + 2);
-            auto at = [&](int c) { return src + (int64_t)(2 * c + (c == c0 ? 1 : 0)) * ROWS * (D + 2); };
-            float mx = -kNone;
-            for (int c = c0 + lane; c <= c1; c += 32) mx = fmaxf(mx, __ldcg(at(c) + D));
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-            float sum[W32], lsum = 0.f;
-#pragma unroll
-            for (int i = 0; i < W32; ++i) sum[i] = 0.f;
+        for (int n = 0; n < ROWS * 16 / THREADS; ++n) {
+            const int r = n * (THREADS / 16) + (tid >> 4), c = tid & 15, row = row0 + r, i = row / a.group;
+            if (i >= a.L) continue;
+            const int64_t out = b * a.o_sb + (hk * a.group + row - i * a.group) * a.o_sh + (int64_t)i * a.o_sr;
+            const float *src = a.part + ((int64_t)2 * c0 * ROWS + r) * S::kPitchP;
+            auto at = [&](int k) { return src + (int64_t)(2 * k + (k == 0 ? 1 : 0)) * ROWS * S::kPitchP; };
+            float mx = -kNone, lsum = 0.f;
 #pragma unroll 4
-            for (int c = c0; c <= c1; ++c) {
-                const float f = ex2(__ldcg(at(c) + D) - mx);
-                lsum = fmaf(f, __ldcg(at(c) + D + 1), lsum);
+            for (int k = 0; k <= c1 - c0; ++k) mx = fmaxf(mx, __ldcg(at(k) + D));
+            float4 sum[NG];
 #pragma unroll
-                for (int i = 0; i < W32; ++i) sum[i] = fmaf(f, __ldcg(at(c) + i * 32 + lane), sum[i]);
+            for (int j = 0; j < NG; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+            for (int k = 0; k <= c1 - c0; ++k) {
+                const float2 ref = __ldcg(reinterpret_cast<const float2 *>(at(k) + D));
+                const float f = ex2(ref.x - mx);
+                lsum = fmaf(f, ref.y, lsum);
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(at(k) + j * 64 + 4 * c));
+                    sum[j].x = fmaf(f, v.x, sum[j].x); sum[j].y = fmaf(f, v.y, sum[j].y); sum[j].z = fmaf(f, v.z, sum[j].z); sum[j].w = fmaf(f, v.w, sum[j].w);
+                }
             }
             const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-            __nv_bfloat16 *o = a.o + b * a.o_sb + (hk * a.group + row - qi * a.group) * a.o_sh + (int64_t)qi * a.o_sr;
 #pragma unroll
-            for (int i = 0; i < W32; ++i) o[i * 32 + lane] = __float2bfloat16_rn(lsum == 0.f ? 0.f : sum[i] * inv);
+            for (int j = 0; j < NG; ++j) put(out, j, c, sum[j], inv);
         }
     }
     if (dead) drain_copies();
@@ -836,7 +861,7 @@ bool kv4_attn_fits(const Kv4AttnProblem &p, const kv4::View &cache)
            p.B * p.Hq < INT32_MAX;
 }
 
-static size_t parts_bytes(const Kv4AttnProblem &p) { return align_up((size_t)sm_count() * 4 * 2 * 8 * row_tiles(p) * (p.D + 2) * 4, 256); }
+static size_t parts_bytes(const Kv4AttnProblem &p) { return align_up((size_t)sm_count() * 4 * 2 * 8 * row_tiles(p) * (p.D + 4) * 4, 256); }
 
 size_t kv4_attn_workspace_bytes(const Kv4AttnProblem &p)
 {
@@ -855,6 +880,11 @@ int launch_kv4_attn(const Kv4AttnProblem &p, const kv4::View &cache, float *scra
     a.B = (int)p.B; a.Hkv = (int)p.Hkv; a.group = (int)(p.Hq / p.Hkv); a.L = (int)p.L; a.kd = (int)p.kd; a.causal = p.causal;
     a.chunks = (int)ceil_div((int64_t)a.group * a.L, 8 * nt);
     a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p.D));
+    auto multiple = [](const void *ptr, int64_t x, int64_t y, int64_t z, size_t of) {
+        return reinterpret_cast<uintptr_t>(ptr) % of == 0 && 2 * x % of == 0 && 2 * y % of == 0 && 2 * z % of == 0;
+    };
+    a.q_vec = multiple(p.q, p.q_sb, p.q_sh, p.q_sr, 16);
+    a.o_pairs = multiple(p.o, p.o_sb, p.o_sh, p.o_sr, 4);
     a.part = scratch;
     a.counters = counters;
     a.status = status;

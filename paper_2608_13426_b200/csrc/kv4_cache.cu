@@ -38,8 +38,8 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
 }
 
 // Eight bf16 columns a lane, eight lanes a step: codes as whole numbers n, step and least value.
-// n is the nearest to the exact quotient (x - m) / s: a product by the reciprocal is off by less than 2^-18, and the exact remainder
-// x - m - n s says where it went to the wrong side of a half or met one (which goes to the even code).
+// The quotient is a product by the reciprocal and one correction by its remainder, which rounds as a division does; a half goes to
+// the even code.  No code is above 15: the step is less than 2^-8 below a fifteenth of the range.
 __device__ __forceinline__ void quantise8(const uint32_t (&w)[4], Eight &n, float &s, float &m)
 {
     // least and (negated) largest value, side by side
@@ -50,52 +50,33 @@ __device__ __forceinline__ void quantise8(const uint32_t (&w)[4], Eight &n, floa
     m = bf16_bits(ends);
     const float hi = -__uint_as_float(ends & 0xffff0000u);
     s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, m), 15.f)));
-    const bool tiny = s < 7.5e-37f;   // too small for a reciprocal
-    const float half = 0.5f * s;
-    const uint64_t inv = both(s > 0.f ? __fdividef(1.f, s) : 0.f), magic = both(12582912.f), minus = both(-12582912.f), step = both(-s), least = both(-m);
+    float r = __fdividef(1.f, s);
+    r = fmaf(fmaf(-s, r, 1.f), r, r);
+    const uint64_t inv = both(r), step = both(-s), least = both(-m), magic = both(12582912.f), minus = both(-12582912.f);
     Eight x;
     widen(Raw8<__nv_bfloat16>{w[0], w[1], w[2], w[3]}, x);
-    bool near = tiny;
-    float e[8], a[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint64_t off = ptx::fadd2(x[i], least);
-        n[i] = ptx::fadd2(ptx::ffma2(off, inv, magic), minus);   // to the nearest whole number
-        ptx::unpack2(off, a[2 * i], a[2 * i + 1]);
-        ptx::unpack2(ptx::ffma2(n[i], step, off), e[2 * i], e[2 * i + 1]);
-        near |= fabsf(e[2 * i]) >= half || fabsf(e[2 * i + 1]) >= half;
+        const uint64_t a = ptx::fadd2(x[i], least), q = fmul2(a, inv);
+        n[i] = ptx::fadd2(ptx::fadd2(ptx::ffma2(ptx::ffma2(q, step, a), inv, q), magic), minus);   // to the nearest whole number
     }
-    if (near && s > 0.f) {
+    if (s < 7.5e-37f) {   // no step, or one too small for a reciprocal
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float v[2];
-            ptx::unpack2(n[i], v[0], v[1]);
+            ptx::unpack2(x[i], v[0], v[1]);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const float r = fabsf(e[2 * i + c]);
-                if (tiny) v[c] = rintf(__fdiv_rn(a[2 * i + c], s));
-                else if (r > half || (r == half && ((int)v[c] & 1))) v[c] += e[2 * i + c] > 0.f ? 1.f : -1.f;
-            }
+            for (int c = 0; c < 2; ++c) v[c] = s > 0.f ? fminf(rintf(__fdiv_rn(__fsub_rn(v[c], m), s)), 15.f) : 0.f;
             n[i] = ptx::pack2(v[0], v[1]);
         }
     }
-    if (s == 0.f)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) n[i] = 0;
 }
 
-// (codes above 15, by the step's rounding, are 15)
-__device__ __forceinline__ uint32_t pack_codes(Eight &n)
+__device__ __forceinline__ uint32_t pack_codes(const Eight &n)   // four at a time are a whole number below 2^16
 {
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        ptx::unpack2(n[i], v[2 * i], v[2 * i + 1]);
-        v[2 * i] = fminf(v[2 * i], 15.f);
-        v[2 * i + 1] = fminf(v[2 * i + 1], 15.f);
-        n[i] = ptx::pack2(v[2 * i], v[2 * i + 1]);
-    }
-    // four at a time are a whole number below 2^16
+    for (int i = 0; i < 4; ++i) ptx::unpack2(n[i], v[2 * i], v[2 * i + 1]);
     const float l = fmaf(fmaf(fmaf(v[3], 16.f, v[2]), 16.f, v[1]), 16.f, v[0]), h = fmaf(fmaf(fmaf(v[7], 16.f, v[6]), 16.f, v[5]), 16.f, v[4]);
     return __byte_perm(__float_as_uint(l + 8388608.f), __float_as_uint(h + 8388608.f), 0x5410);
 }
@@ -105,7 +86,10 @@ __device__ __forceinline__ void dequantise8(uint32_t codes, uint32_t pair, Eight
 {
     const uint64_t s = both(bf16_bits(pair)), m = both(__uint_as_float(pair & 0xffff0000u));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = ptx::ffma2(s, ptx::pack2((float)(codes >> (8 * i) & 15u), (float)(codes >> (8 * i + 4) & 15u)), m);
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t n = ptx::pack2(__uint_as_float((codes >> (8 * i) & 15u) | 0x4b000000u), __uint_as_float((codes >> (8 * i + 4) & 15u) | 0x4b000000u));
+        x[i] = ptx::ffma2(s, ptx::fadd2(n, both(-8388608.f)), m);
+    }
 }
 
 // Which token a lane's row is, and where it lies.
@@ -232,7 +216,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv4_read_kernel(const __grid_cons
     const int key = kv4::key_word(D, p.t, chunk), value = kv4::value_word(D, p.t, chunk), pair = kv4::key_pair_word(D, p.t, chunk >> 3);
     TO *kh = static_cast<TO *>(a.k.dst) + p.b * a.k.d_b + p.i * a.k.d_r + p.h0 * a.k.d_h + p.col;
     TO *vh = static_cast<TO *>(a.v.dst) + p.b * a.v.d_b + p.i * a.v.d_r + p.h0 * a.v.d_h + p.col;
-#pragma unroll 2
+#pragma unroll 4
     for (int h = p.h0; h < p.h1; ++h) {
         Eight k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
         if (base != nullptr) {
