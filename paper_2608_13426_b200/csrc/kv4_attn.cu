@@ -35,6 +35,7 @@ namespace {
 constexpr int kWarps = 4, kPair = 2 * kv4::kBlock;   // warps of a CTA; tokens of a warp's turn
 constexpr int kFixed = 12, kLeast = kFixed + 8;      // pairs that a job's fixed part counts as; the least share of a CTA
 constexpr int kCut = 1;                              // a job of that many shares is cut into pieces of its own
+constexpr int kMeet = 16;                             // CTAs whose parts are added up in one step
 constexpr float kTopWeight = 16384.f, kTop = 6.f, kLeastStep = 8.2718061e-25f;   // 2^14, log2 of 2^6, 2^-80: see above; smaller steps weigh as that
 constexpr float kNone = 1e30f;                       // minus the reference of a row that has seen no key
 
@@ -146,7 +147,9 @@ __device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int share)  
 template <int W32>
 __global__ void __launch_bounds__(128) kv4_features_kernel(const __grid_constant__ AttnArgs a, uint32_t *kept, int32_t *idx_feat)
 {
-    pdl_wait();
+    // The attention may start once everything before this kernel is complete: it waits for the masks only where it reads them
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int64_t job = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), Hq = (int64_t)a.Hkv * a.group;
     if (job >= a.B * Hq) return;
@@ -203,7 +206,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     using S = Shape<D, NT>;
     constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32, THREADS = kWarps * 32;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int s_scan[2][kWarps], s_begin[2], s_pending[2][5], abort_flag, s_last[2];
+    __shared__ int s_scan[2][kWarps], s_begin[2], s_pending[2][5], abort_flag, s_last;
     int64_t *row_out = reinterpret_cast<int64_t *>(smem + S::kOffOut);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * ST * S::kPairBytes, bars = smem_u32(smem) + S::kOffBar + warp * ST * 8;
@@ -218,7 +221,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     if (tid == 0) abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
-    pdl_wait();
+    if (a.kept == nullptr) pdl_wait();   // (behind the features kernel: what comes before that is complete)
 
     // ---- this CTA's share
     Job cur;
@@ -244,7 +247,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         if (a.B > THREADS) {
             cur.b = b0 + tid;
             if (cur.b < a.B) job_sequence<ROWS>(a, cur, share);
-        } else if (cur.b < a.B && cur.len > 0 && cur.each >= share) {
+        } else if (cur.b < a.B && cur.len > 0 && cur.each / kCut >= share) {
             cur.each = 0;
         }
         mine[0] = mine[1] = 0;
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             }
         }
     };
-    load_q();
+    if (a.kept == nullptr) load_q();
 
     // ---- the warp's loads: pairs first + warp, + 4, .. of every part, ST of them under way
     Job pc = cur;
@@ -420,6 +423,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     };
     settle();
     for (int i = 0; i < ST; ++i) request();
+    if (a.kept != nullptr) {
+        pdl_wait();
+        load_q();
+    }
 
     // columns 64 j + 8 (2 (c % 4)) + 2 (c / 4), the next, and those 8 on, of an output row
     auto put = [&](int64_t row, int j, int c, float4 v, float inv) {
@@ -787,51 +794,71 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         if (start < u_end) job_next<ROWS>(a, cur, share);
     }
 
-    // ---- jobs that other CTAs work on too: whichever comes last adds the parts up
-    __syncthreads();
-    if (tid < 2) {
-        const int c0 = s_pending[tid][0];
-        s_last[tid] = 0;
-        if (c0 >= 0) {
-            const unsigned n = (unsigned)(s_pending[tid][1] - c0);
-            __threadfence();   // (fences are cumulative: this one stands for all that the barrier has ordered before it)
-            s_last[tid] = atomicInc(a.counters + c0, n) == n;
-            __threadfence();
-        }
-    }
+    // ---- jobs that other CTAs work on too: whichever comes last adds the parts up, in two steps where there are more than kMeet or so.
     __syncthreads();
     for (int k = 0; k < 2; ++k) {
-        if (!s_last[k]) continue;
-        const int c0 = s_pending[k][0], c1 = s_pending[k][1], row0 = s_pending[k][4];
+        const int c0 = s_pending[k][0];
+        if (c0 < 0) continue;
+        const int n = s_pending[k][1] - c0 + 1, row0 = s_pending[k][4];
         const int64_t b = s_pending[k][2], hk = s_pending[k][3];
+        // (no group is the job's last CTA alone, in which another job may begin: a group's counter is that of its first CTA)
+        const int groups = (n - 2) / kMeet + 1, group = min(((int)blockIdx.x - c0) / kMeet, groups - 1);
+        int first_part = c0 + group * kMeet, parts = group == groups - 1 ? n - group * kMeet : kMeet, apart = 1;
+        unsigned *counter = a.counters + first_part;
+        while (true) {
+            if (tid == 0) {
+                __threadfence();   // (fences are cumulative: this one stands for all that the barrier has ordered before it)
+                s_last = atomicInc(counter, (unsigned)parts - 1u) == (unsigned)parts - 1u;
+                __threadfence();
+            }
+            __syncthreads();
+            if (!s_last) break;
+            const bool final = apart > 1 || groups == 1;
 #pragma unroll
-        for (int n = 0; n < ROWS * 16 / THREADS; ++n) {
-            const int r = n * (THREADS / 16) + (tid >> 4), c = tid & 15, row = row0 + r, i = row / a.group;
-            if (i >= a.L) continue;
-            const int64_t out = b * a.o_sb + (hk * a.group + row - i * a.group) * a.o_sh + (int64_t)i * a.o_sr;
-            const float *src = a.part + ((int64_t)2 * c0 * ROWS + r) * S::kPitchP;
-            auto at = [&](int k) { return src + (int64_t)(2 * k + (k == 0 ? 1 : 0)) * ROWS * S::kPitchP; };
-            float mx = -kNone, lsum = 0.f;
-#pragma unroll 4
-            for (int k = 0; k <= c1 - c0; ++k) mx = fmaxf(mx, __ldcg(at(k) + D));
-            float4 sum[NG];
+            for (int t = 0; t < ROWS * 16 / THREADS; ++t) {
+                const int r = t * (THREADS / 16) + (tid >> 4), c = tid & 15, row = row0 + r, i = row / a.group;
+                if (i >= a.L) continue;
+                auto at = [&](int p) {
+                    const int cta = first_part + p * apart;
+                    return a.part + ((int64_t)(2 * cta + (cta == c0 ? 1 : 0)) * ROWS + r) * S::kPitchP;
+                };
+                float mx = -kNone, lsum = 0.f;
+                float4 sum[NG];
 #pragma unroll
-            for (int j = 0; j < NG; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-            for (int k = 0; k <= c1 - c0; ++k) {
-                const float2 ref = __ldcg(reinterpret_cast<const float2 *>(at(k) + D));
-                const float f = ex2(ref.x - mx);
-                lsum = fmaf(f, ref.y, lsum);
+                for (int j = 0; j < NG; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int p = 0; p < parts; ++p) mx = fmaxf(mx, __ldcg(at(p) + D));
+#pragma unroll (NG <= 2 ? 4 : 2)
+                for (int p = 0; p < parts; ++p) {
+                    const float2 ref = __ldcg(reinterpret_cast<const float2 *>(at(p) + D));
+                    const float f = ex2(ref.x - mx);
+                    lsum = fmaf(f, ref.y, lsum);
 #pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(at(k) + j * 64 + 4 * c));
-                    sum[j].x = fmaf(f, v.x, sum[j].x); sum[j].y = fmaf(f, v.y, sum[j].y); sum[j].z = fmaf(f, v.z, sum[j].z); sum[j].w = fmaf(f, v.w, sum[j].w);
+                    for (int j = 0; j < NG; ++j) {
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(at(p) + j * 64 + 4 * c));
+                        sum[j].x = fmaf(f, v.x, sum[j].x); sum[j].y = fmaf(f, v.y, sum[j].y); sum[j].z = fmaf(f, v.z, sum[j].z); sum[j].w = fmaf(f, v.w, sum[j].w);
+                    }
+                }
+                if (final) {
+                    const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+                    const int64_t out = b * a.o_sb + (hk * a.group + row - i * a.group) * a.o_sh + (int64_t)i * a.o_sr;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) put(out, j, c, sum[j], inv);
+                } else {   // (a row's sixteen threads are of one warp: all have read before any writes)
+                    __syncwarp(0xffffu << (lane & 16));
+                    float *to = at(0);
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) *reinterpret_cast<float4 *>(to + j * 64 + 4 * c) = sum[j];
+                    if (c == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(mx, lsum);
                 }
             }
-            const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-#pragma unroll
-            for (int j = 0; j < NG; ++j) put(out, j, c, sum[j], inv);
+            if (final) break;
+            __syncthreads();
+            first_part = c0;
+            apart = kMeet;
+            parts = groups;
+            counter = a.counters + gridDim.x + c0 / kMeet;   // (the first CTAs of two such jobs are more than kMeet apart)
         }
+        __syncthreads();
     }
     if (dead) drain_copies();
 }
@@ -847,7 +874,9 @@ int launch(const AttnArgs &a, cudaStream_t stream)
     static PerDeviceOnce configured;
     if (cudaError_t e = configured.smem(S::kSmem, kern)) return fail(RMM_ERR_CUDA, "kv4_attn: cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     prof_begin("kv4_attn_kernel", stream);
-    launch_kernel(kern, dim3((unsigned)(sm_count() * S::kCtas)), dim3(kWarps * 32), S::kSmem, stream, 1, a);
+    // (counters: one a CTA, one for kMeet of them)
+    const int64_t ctas = (int64_t)sm_count() * S::kCtas, most = (kHeaderCounters - 4) * kMeet / (kMeet + 1) - 1;
+    launch_kernel(kern, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kWarps * 32), S::kSmem, stream, 1, a);
     return check_launch("kv4_attn_kernel", stream);
 }
 

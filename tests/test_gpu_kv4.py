@@ -217,6 +217,12 @@ def test_many_short_and_some_long_sequences():
     check_attn(lengths, 8, 2, 128, 16, 3, new=[i % 4 for i in range(70)], rho_d=0.5, seed=2)
 
 
+@pytest.mark.parametrize("pairs", [308, 328, 348, 629, 648, 668, 1250])
+def test_one_job_over_many_blocks_of_the_grid(pairs):
+    """Jobs cut into 16, 17, 18, 32, 33, 34 and more pieces, whose sums meet in one step or in two."""
+    check_attn([pairs * 32 - 5], 3, 1, 64, 64, 1, seed=pairs)
+
+
 @pytest.mark.parametrize("q_scale, k_scale", [(30.0, 30.0), (1e-6, 1.0), (1e4, 1e-3), (1e-12, 1e12)])
 def test_logits_of_any_size(q_scale, k_scale):
     check_attn([200, 77], 4, 2, 128, 16, 2, q_scale=q_scale, k_scale=k_scale, seed=3)
