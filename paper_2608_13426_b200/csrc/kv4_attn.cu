@@ -15,10 +15,11 @@
 //     keys (or columns of V): the group's rows fill what 128-row tcgen05 tiles would pad.
 // Lengths live on the device, so nothing is planned on the host and a captured call follows them: every CTA works its share out.
 // Work is counted in pairs of 16-token blocks; a job (sequence, kv head, row tile) counts kFixed pairs more than it has, for what a
-// CTA spends on it outside the keys.  A job of at least a CTA's equal share S is cut into floor(its cost / S) equal pieces, a CTA
-// each; the others form one axis that the remaining CTAs cut evenly.  Within a CTA every warp takes every fourth pair through a ring
-// of its own, filled by bulk copies of whole blocks, which runs on across jobs.  A job that is not one CTA's alone leaves its sums in the
-// workspace; the last CTA of it to arrive adds them up, in order.
+// CTA spends on it outside the keys, and kMeeting more where its sums meet those of other CTAs.  For a limit T, a job that counts more is
+// cut into the fewest equal pieces that do not, a CTA each; the others lie on one axis of which the remaining CTAs have equal stretches, and
+// each does the jobs that begin in its own.  T is the least of a few multiples of the equal share for which there are CTAs enough.
+// Within a CTA every warp takes every fourth pair through a ring of its own, filled by bulk copies of whole blocks, which runs on
+// across jobs.  Pieces leave their sums in the workspace; the last CTA of a job to arrive adds them up.
 #include <math.h>
 
 #include <cuda_fp16.h>
@@ -33,8 +34,10 @@ namespace rmm {
 namespace {
 
 constexpr int kWarps = 4, kPair = 2 * kv4::kBlock;   // warps of a CTA; tokens of a warp's turn
-constexpr int kFixed = 12, kLeast = kFixed + 8;      // pairs that a job's fixed part counts as; the least share of a CTA
-constexpr int kCut = 1;                              // a job of that many shares is cut into pieces of its own
+constexpr int kFixed = 8, kMeeting = 6;               // pairs that a job's fixed part counts as, and the meeting of its parts
+constexpr int kLeast = kFixed + 2 * kMeeting;         // the least limit: two pieces take no less time than a job of that size
+constexpr int kLimits = 8;                            // limits that are tried, in sixteenths of the equal share
+__device__ constexpr int kLimit[kLimits] = {16, 17, 18, 20, 23, 26, 30, 36};
 constexpr int kMeet = 16;                             // CTAs whose parts are added up in one step
 constexpr float kTopWeight = 16384.f, kTop = 6.f, kLeastStep = 8.2718061e-25f;   // 2^14, log2 of 2^6, 2^-80: see above; smaller steps weigh as that
 constexpr float kNone = 1e30f;                       // minus the reference of a row that has seen no key
@@ -48,7 +51,7 @@ struct AttnArgs {
     int causal;
     float scale_log2;
     const uint32_t *kept;     // [B][Hq][D / 32] bit masks of the kept features, or NULL: all
-    float *part;              // [2 CTAs][rows][D + 4]: sums in the order of the merge, then reference and sum of weights
+    float *part;              // [CTAs][rows][D + 4]: sums in the order of the merge, then reference and sum of weights
     int q_vec, o_pairs;       // rows of Q on 16-byte boundaries, of O on 4-byte ones
     unsigned *counters;
     int *status;
@@ -115,20 +118,20 @@ struct Job {
 };
 
 template <int ROWS>
-__device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c, int share)
+__device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c, int limit)
 {
     kv4::sequence(a.cache, c.b, c.len, c.rows, a.status);
     c.nb = (c.len + kPair - 1) / kPair;
     c.valid = (c.rows * a.group + ROWS - 1) / ROWS;
-    c.each = c.len == 0 ? 1 : ((c.nb + kFixed) / kCut >= share ? 0 : c.nb + kFixed);
+    c.each = c.len == 0 ? 1 : (c.nb + kFixed > limit ? 0 : c.nb + kFixed);
 }
 __device__ __forceinline__ int head_cost(const AttnArgs &a, const Job &c) { return c.valid * c.each + a.chunks - c.valid; }
-__device__ __forceinline__ int pieces_of(const Job &c, int share)   // of a reading job that is cut
+__device__ __forceinline__ int pieces_of(const Job &c, int limit)   // of a reading job that is cut
 {
-    return min((c.nb + kFixed) / share, max(1, c.nb / kWarps));
+    return max(1, min((int)ceilf(__fdividef((float)c.nb, (float)(limit - kFixed - kMeeting))), c.nb / kWarps));
 }
 template <int ROWS>
-__device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int share)   // the next one that counts
+__device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int limit)   // the next one that counts
 {
     ++c.chunk;
     while (true) {
@@ -138,7 +141,7 @@ __device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int share)  
         if (++c.hk < a.Hkv && head_cost(a, c) > 0) continue;
         c.hk = 0;
         if (++c.b >= a.B) return;
-        job_sequence<ROWS>(a, c, share);
+        job_sequence<ROWS>(a, c, limit);
     }
 }
 
@@ -206,7 +209,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     using S = Shape<D, NT>;
     constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32, THREADS = kWarps * 32;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int s_scan[2][kWarps], s_begin[2], s_pending[2][5], abort_flag, s_last;
+    __shared__ Job s_cur, s_pc[kWarps];   // the job at hand, and the one that a warp asks for (kept out of the registers of the loop over the keys)
+    __shared__ int s_need[kLimits][kWarps], s_scan[2][kWarps], s_begin[2], abort_flag, s_last;
     int64_t *row_out = reinterpret_cast<int64_t *>(smem + S::kOffOut);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * ST * S::kPairBytes, bars = smem_u32(smem) + S::kOffBar + warp * ST * 8;
@@ -241,18 +245,53 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         for (int w = 0; w < kWarps; ++w) total += s_scan[0][w];
     }
     const int share = max(kLeast, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+    int limit = share;
+    {
+        int need[kLimits];   // CTAs that a limit asks for, in 64ths (many more than there are: 2^14 of them)
+#pragma unroll
+        for (int k = 0; k < kLimits; ++k) need[k] = 0;
+        for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+            if (a.B > THREADS) {
+                cur.b = b0 + tid;
+                if (cur.b < a.B) job_sequence<ROWS>(a, cur, INT32_MAX);
+            }
+            if (cur.b < a.B) {
+#pragma unroll
+                for (int k = 0; k < kLimits; ++k) {
+                    const int t = share * kLimit[k] / 16;
+                    const bool cut = cur.len > 0 && cur.each > t;
+                    const float ctas = cut ? (float)cur.valid * (float)pieces_of(cur, t) : 0.f;
+                    const float rest = (float)(cut ? a.chunks - cur.valid : head_cost(a, cur));
+                    need[k] = min(need[k] + (int)fminf(ceilf(64.f * (float)a.Hkv * (ctas + __fdividef(rest, (float)t))), 1048576.f), 1048576);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kLimits; ++k) {
+            const int v = warp * 32 < a.B ? __reduce_add_sync(0xffffffffu, need[k]) : 0;
+            if (lane == 0) s_need[k][warp] = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = kLimits - 1; k >= 0; --k) {
+            int v = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) v += s_need[k][w];
+            if (k == kLimits - 1 || v <= 64 * (int)gridDim.x) limit = share * kLimit[k] / 16;
+        }
+    }
     // CTAs with a piece of a job, and what the other jobs count: this thread's sequence, the sequences up to it, all
     int mine[2] = {0, 0}, upto[2] = {0, 0}, sum[2] = {0, 0};
     auto scan = [&](int b0) {
         if (a.B > THREADS) {
             cur.b = b0 + tid;
-            if (cur.b < a.B) job_sequence<ROWS>(a, cur, share);
-        } else if (cur.b < a.B && cur.len > 0 && cur.each / kCut >= share) {
+            if (cur.b < a.B) job_sequence<ROWS>(a, cur, limit);
+        } else if (cur.b < a.B && cur.len > 0 && cur.each > limit) {
             cur.each = 0;
         }
         mine[0] = mine[1] = 0;
         if (cur.b < a.B) {
-            mine[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, share) : 0;
+            mine[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, limit) : 0;
             mine[1] = a.Hkv * head_cost(a, cur);
         }
         upto[0] = mine[0];
@@ -287,12 +326,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         axis += sum[1];
     }
     const bool piece = (int)blockIdx.x < n_pieces;
-    const int ctas = min((int)gridDim.x - n_pieces, (axis + kLeast - 1) / kLeast), cta = (int)blockIdx.x - n_pieces;   // of the axis
-    if (cta >= ctas) return;
-    // equal shares: the first `rest` CTAs of the axis have `each` + 1, the others `each`
-    const int each = ctas > 0 ? axis / ctas : 0, rest = axis - each * ctas;
-    auto owner = [&](int at) { return at < rest * (each + 1) ? at / (each + 1) : rest + (at - rest * (each + 1)) / each; };
-    int u_begin = piece ? (int)blockIdx.x : each * cta + min(cta, rest), u_end = piece ? 0 : u_begin + each + (cta < rest ? 1 : 0);
+    const int ctas = min((int)gridDim.x - n_pieces, axis / (kFixed + 1) + 1), cta = (int)blockIdx.x - n_pieces;   // of the axis
+    if (cta >= ctas || (!piece && axis == 0)) return;
+    const int each = axis / max(1, ctas), rest = axis - each * ctas;   // the first `rest` stretches have `each` + 1, the others `each`
+    int u_begin = piece ? (int)blockIdx.x : each * cta + min(cta, rest), u_end = u_begin + each + (cta < rest ? 1 : 0);
+    if (u_begin == u_end && !piece) return;
     for (int b0 = 0, base = 0; b0 < a.B; b0 += THREADS) {
         if (a.B > THREADS) scan(b0);
         const int i = piece ? 0 : 1;
@@ -304,19 +342,19 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     }
     __syncthreads();
 
-    int start, piece0 = 0, pieces = 1;   // where the current job begins on the axis; a piece's job: its first CTA, its CTAs
+    int start = 0, first_pair = 0, end_pair = INT32_MAX, piece0 = 0, pieces = 1;   // where the job begins on the axis; a piece: its pairs, the job's first CTA, its CTAs
     cur.b = s_begin[0];
-    job_sequence<ROWS>(a, cur, share);
+    job_sequence<ROWS>(a, cur, limit);
     if (piece) {
-        pieces = pieces_of(cur, share);
+        pieces = pieces_of(cur, limit);
         const int off = u_begin - s_begin[1], job = off / pieces, k = off - job * pieces, nb = cur.nb / pieces, more = cur.nb - nb * pieces;
         piece0 = (int)blockIdx.x - k;
         cur.hk = job / cur.valid;
         cur.chunk = job - cur.hk * cur.valid;
-        cur.each = cur.nb + kFixed;   // alone on an axis of its own
-        start = 0;
-        u_begin = kFixed + nb * k + min(k, more);
-        u_end = u_begin + nb + (k < more ? 1 : 0);
+        cur.each = 1;   // alone on an axis of its own
+        u_end = 1;
+        first_pair = nb * k + min(k, more);
+        end_pair = first_pair + nb + (k < more ? 1 : 0);
     } else {
         const int per_head = head_cost(a, cur);
         int off = u_begin - s_begin[1];
@@ -325,10 +363,15 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         const bool in = off < cur.valid * cur.each;
         cur.chunk = in ? off / cur.each : cur.valid + off - cur.valid * cur.each;
         start = u_begin - (in ? off - cur.chunk * cur.each : 0);
+        if (start < u_begin) {   // that job is the CTA's before
+            start += cur.cost();
+            if (start >= u_end) return;
+            job_next<ROWS>(a, cur, limit);
+        }
     }
-    // the pairs of the job at `at` that are this CTA's
-    auto first_pair = [&](int at) { return max(0, u_begin - at - kFixed); };
-    auto last_pair = [&](const Job &c, int at) { return min(c.nb, u_end - at - kFixed); };
+    if (tid == 0) s_cur = cur;
+    if (lane == 0) s_pc[warp] = cur;
+    __syncthreads();
 
     // ---- Q of a row tile: row i * group + h of the kv head's rows (asked for before the keys are, whose page numbers come first).
     // D / 8 lanes share a row, eight columns each.
@@ -337,6 +380,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     uint32_t q_kept[QT];
     auto q_row = [&](int k) { return (k * THREADS + tid) / QL; };
     auto load_q = [&]() {
+        const Job cur = s_cur;
         const int row0 = cur.chunk * ROWS, nrows = min(ROWS, cur.rows * a.group - row0), c = tid % QL;
 #pragma unroll
         for (int k = 0; k < QT; ++k) {
@@ -353,27 +397,28 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     if (a.kept == nullptr) load_q();
 
     // ---- the warp's loads: pairs first + warp, + 4, .. of every part, ST of them under way
-    Job pc = cur;
     int p_start = start, p_t = 0, p_end = 0, p_k = 64, p_slot = 0;
-    uint64_t from0 = 0, from1 = 0;   // lanes hold where the blocks of the next 32 pairs lie,
-    int p_tokens = 0;                // and their tokens (of the first block, + 256 x of the second; 0: a page outside the pool)
+    uint64_t from0 = 0;              // lanes hold where the blocks of the next 32 pairs lie (the second's page, where that is another),
+    int page1 = 0, p_tokens = 0;     // and their tokens (of the first block, + 256 x of the second; 0: a page outside the pool)
     const bool split = a.cache.page_shift == 0;   // the blocks of a pair lie in two pages
     auto window = [&]() {
-        const int t = p_t + lane * kWarps, left = pc.len - t * kPair;
+        const int b = s_pc[warp].b;
+        const int t = p_t + lane * kWarps, left = s_pc[warp].len - t * kPair;
         int n0 = max(0, min(left, kv4::kBlock)), n1 = max(0, min(left - kv4::kBlock, kv4::kBlock));
-        const int32_t *row = a.cache.pages + pc.b * a.cache.pages_stride;
-        const uint8_t *head = a.cache.pool + pc.hk * a.cache.head_stride;
+        const int32_t *row = a.cache.pages + b * a.cache.pages_stride;
         const int i0 = n0 > 0 ? __ldg(row + (2 * t >> a.cache.page_shift)) : 0, i1 = split && n1 > 0 ? __ldg(row + 2 * t + 1) : i0;
         const bool good0 = i0 >= 0 && i0 < a.cache.n_pages, good1 = i1 >= 0 && i1 < a.cache.n_pages;
         if (t < p_end && (!good0 || !good1)) atomicExch(a.status, (int)RMM_ERR_BOUNDS);
         if (!good0) n0 = 0;
         if (!good1) n1 = 0;
-        from0 = reinterpret_cast<uint64_t>(head + (int64_t)i0 * a.cache.page_stride + (int64_t)(2 * t & ((1 << a.cache.page_shift) - 1)) * S::kBlockBytes);
-        from1 = reinterpret_cast<uint64_t>(head + (int64_t)i1 * a.cache.page_stride);
+        from0 = reinterpret_cast<uint64_t>(a.cache.pool + s_pc[warp].hk * a.cache.head_stride + (int64_t)i0 * a.cache.page_stride +
+                                           (int64_t)(2 * t & ((1 << a.cache.page_shift) - 1)) * S::kBlockBytes);
+        page1 = i1;
         p_tokens = n0 | n1 << 8;
         p_k = 0;
     };
     auto settle = [&]() {   // from the end of a part on to the next pair that has something to load
+        Job pc = s_pc[warp];
         while (true) {
             if (p_k != 64) {
                 p_start += pc.cost();
@@ -381,20 +426,23 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     p_t = p_end = 0;
                     return;
                 }
-                job_next<ROWS>(a, pc, share);
+                job_next<ROWS>(a, pc, limit);
             }
-            p_end = pc.reads() ? last_pair(pc, p_start) : 0;
-            p_t = first_pair(p_start) + warp;
+            p_end = pc.reads() ? min(pc.nb, end_pair) : 0;
+            p_t = first_pair + warp;
             p_k = 32;
             if (p_t < p_end) break;
         }
+        __syncwarp();
+        if (lane == 0) s_pc[warp] = pc;
+        __syncwarp();
         window();
     };
     auto request = [&]() {
         if (p_t >= p_end) return;
         if (lane == p_k) {   // the lane that knows the pair
             const int n = p_tokens;
-            const uint64_t src0 = from0, src1 = from1;
+            const uint64_t src0 = from0;
             const uint32_t bar = bars + 8 * p_slot, dst = ring + (uint32_t)p_slot * S::kPairBytes;
             const uint32_t b0 = n & 255 ? S::kBlockBytes : 0, b1 = n >> 8 ? S::kBlockBytes : 0;
             auto copy = [&](uint32_t to, uint64_t from, uint32_t bytes) {
@@ -411,7 +459,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     copy(dst, src0, b0 + b1);
                 } else {
                     if (b0 > 0) copy(dst, src0, b0);
-                    if (b1 > 0) copy(dst + S::kBlockBytes, src1, b1);
+                    if (b1 > 0)
+                        copy(dst + S::kBlockBytes, reinterpret_cast<uint64_t>(a.cache.pool + s_pc[warp].hk * a.cache.head_stride + (int64_t)page1 * a.cache.page_stride), b1);
                 }
             }
         }
@@ -445,16 +494,18 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     int slot = 0;
     uint32_t phases = 0;
     bool dead = false, first = true;
-    if (tid < 2) s_pending[tid][0] = -1;
     while (start < u_end) {
-        const bool reads = cur.reads();
-        const int t0 = reads ? first_pair(start) : 0, t1 = reads ? last_pair(cur, start) : 1;
-        if (t1 > t0) {
-            const int row0 = cur.chunk * ROWS, nrows = max(0, min(ROWS, cur.rows * a.group - row0));
-            const bool whole = !reads || (t0 == 0 && t1 == cur.nb);
-
+        const bool reads = s_cur.reads();
+        const int t0 = first_pair, t1 = min(s_cur.nb, end_pair), cost = s_cur.cost();
+        {
             // ---- Q scaled to fp16
             if (!first) load_q();
+            int vis_least;
+            {
+            const Job cur = s_cur;
+            const int row0 = cur.chunk * ROWS, nrows = max(0, min(ROWS, cur.rows * a.group - row0));
+            // the first row's keys are the fewest
+            vis_least = nrows == 0 ? 0 : (a.causal ? max(0, min(cur.len, cur.len - cur.rows + row0 / a.group + 1)) : cur.len);
 #pragma unroll
             for (int k = 0; k < QT; ++k) {
                 const int r = q_row(k), c = tid % QL;
@@ -487,9 +538,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     row_out[r] = i < a.L ? cur.b * a.o_sb + ((int64_t)cur.hk * a.group + row - i * a.group) * a.o_sh + (int64_t)i * a.o_sr : -1;
                 }
             }
+            }
             __syncthreads();
             float cq[NT][2], qsum[NT][2][NG], nm[NT][2], l[NT][2], low[NT][2][NG], o[NT][D / 16][4];   // nm: minus the reference
-            int vis[NT][2], vis_least = cur.len;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -500,7 +551,6 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                 for (int e = 0; e < 2; ++e) {
                     const int r = nt * 8 + 2 * t4 + e;
                     cq[nt][e] = row_scale[r];
-                    vis[nt][e] = row_vis[r];
                     nm[nt][e] = kNone;
                     l[nt][e] = 0.f;
 #pragma unroll
@@ -510,7 +560,6 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     }
                 }
             }
-            for (int r = 0; r < nrows; ++r) vis_least = min(vis_least, row_vis[r]);
 
             // One pair of blocks.  EDGE: some of its tokens are none, or not seen by every row.
             auto pair = [&](const uint8_t *blk, int t, int held, auto edge_tag) {
@@ -602,7 +651,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                                 for (int c = 0; c < 2; ++c)
-                                    if (g + 8 * e >= n || t * kPair + f * kv4::kBlock + g + 8 * e >= vis[nt][c]) x[f][nt][2 * e + c] = -INFINITY;
+                                    if (g + 8 * e >= n || t * kPair + f * kv4::kBlock + g + 8 * e >= row_vis[nt * 8 + 2 * t4 + c]) x[f][nt][2 * e + c] = -INFINITY;
                         }
                     }
                 // -- weights
@@ -725,6 +774,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     }
                 }
             __syncthreads();
+            const int row0 = s_cur.chunk * ROWS, nrows = s_cur.rows * a.group - row0;
             if (tid < ROWS) {
                 float mx = -kNone, sum = 0.f;
 #pragma unroll
@@ -740,7 +790,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                 tot[tid * 3 + 1] = sum;
                 tot[tid * 3 + 2] = sum == 0.f ? 0.f : 1.f / sum;   // (0: the row sees no key; a NaN stays one)
             }
-            float *part = a.part + (int64_t)(2 * blockIdx.x + (t0 == 0 ? 1 : 0)) * ROWS * S::kPitchP;
+            float *part = a.part + (int64_t)blockIdx.x * ROWS * S::kPitchP;
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
                 if (j > 0) __syncthreads();
@@ -765,7 +815,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                         const float4 v = *reinterpret_cast<const float4 *>(merge + (w * ROWS + r) * S::kPitchM + 4 * c);
                         sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
                     }
-                    if (whole) {
+                    if (pieces == 1) {
                         put(row_out[r], j, c, sum, tot[r * 3 + 2]);
                     } else {
                         *reinterpret_cast<float4 *>(part + r * S::kPitchP + j * 64 + 4 * c) = sum;
@@ -775,35 +825,26 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             }
             __syncthreads();
 
-            if (!whole && tid == 0) {   // other CTAs work on this job too: the first and last of them are
-                int c0 = piece0, c1 = piece0 + pieces - 1;
-                if (!piece) {
-                    c0 = n_pieces + owner(start + kFixed);   // of its first and last pair
-                    c1 = n_pieces + owner(start + kFixed + cur.nb - 1);
-                }
-                int *to = s_pending[t0 == 0 ? 1 : 0];
-                to[0] = c0;
-                to[1] = c1;
-                to[2] = cur.b;
-                to[3] = cur.hk;
-                to[4] = row0;
-            }
         }
         first = false;
-        start += cur.cost();
-        if (start < u_end) job_next<ROWS>(a, cur, share);
+        start += cost;
+        if (start < u_end) {
+            __syncthreads();
+            if (tid == 0) {
+                Job next = s_cur;
+                job_next<ROWS>(a, next, limit);
+                s_cur = next;
+            }
+            __syncthreads();
+        }
     }
 
-    // ---- jobs that other CTAs work on too: whichever comes last adds the parts up, in two steps where there are more than kMeet or so.
-    __syncthreads();
-    for (int k = 0; k < 2; ++k) {
-        const int c0 = s_pending[k][0];
-        if (c0 < 0) continue;
-        const int n = s_pending[k][1] - c0 + 1, row0 = s_pending[k][4];
-        const int64_t b = s_pending[k][2], hk = s_pending[k][3];
-        // (no group is the job's last CTA alone, in which another job may begin: a group's counter is that of its first CTA)
-        const int groups = (n - 2) / kMeet + 1, group = min(((int)blockIdx.x - c0) / kMeet, groups - 1);
-        int first_part = c0 + group * kMeet, parts = group == groups - 1 ? n - group * kMeet : kMeet, apart = 1;
+    // ---- a job that other CTAs work on too: whichever comes last adds the parts up, in two steps where there are more than kMeet or so
+    if (pieces > 1) {
+        const int row0 = s_cur.chunk * ROWS;
+        const int64_t b = s_cur.b, hk = s_cur.hk;
+        const int groups = (pieces - 2) / kMeet + 1, group = min(((int)blockIdx.x - piece0) / kMeet, groups - 1);   // (none of one CTA)
+        int first_part = piece0 + group * kMeet, parts = group == groups - 1 ? pieces - group * kMeet : kMeet, apart = 1;
         unsigned *counter = a.counters + first_part;
         while (true) {
             if (tid == 0) {
@@ -820,7 +861,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                 if (i >= a.L) continue;
                 auto at = [&](int p) {
                     const int cta = first_part + p * apart;
-                    return a.part + ((int64_t)(2 * cta + (cta == c0 ? 1 : 0)) * ROWS + r) * S::kPitchP;
+                    return a.part + ((int64_t)cta * ROWS + r) * S::kPitchP;
                 };
                 float mx = -kNone, lsum = 0.f;
                 float4 sum[NG];
@@ -853,12 +894,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             }
             if (final) break;
             __syncthreads();
-            first_part = c0;
+            first_part = piece0;
             apart = kMeet;
             parts = groups;
-            counter = a.counters + gridDim.x + c0 / kMeet;   // (the first CTAs of two such jobs are more than kMeet apart)
+            counter = a.counters + gridDim.x + piece0 / kMeet;   // (the first CTAs of two such jobs are more than kMeet apart)
         }
-        __syncthreads();
     }
     if (dead) drain_copies();
 }
@@ -890,7 +930,7 @@ bool kv4_attn_fits(const Kv4AttnProblem &p, const kv4::View &cache)
            p.B * p.Hq < INT32_MAX;
 }
 
-static size_t parts_bytes(const Kv4AttnProblem &p) { return align_up((size_t)sm_count() * 4 * 2 * 8 * row_tiles(p) * (p.D + 4) * 4, 256); }
+static size_t parts_bytes(const Kv4AttnProblem &p) { return align_up((size_t)sm_count() * 4 * 8 * row_tiles(p) * (p.D + 4) * 4, 256); }
 
 size_t kv4_attn_workspace_bytes(const Kv4AttnProblem &p)
 {
