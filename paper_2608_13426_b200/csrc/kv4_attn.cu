@@ -73,7 +73,8 @@ struct Shape {
     static constexpr int kOffTot = kOffRow + kRows * (2 + kGroups) * 4;        // [row]: reference and sum of the CTA, one over the sum
     static constexpr int kOffBar = (kOffTot + kRows * 12 + 15) / 16 * 16;      // barriers, then the tokens of each ring entry
     static constexpr int kSmem = kOffBar + kWarps * kStages * 12;
-    static_assert((kSmem + 1280) * kCtas <= 227 * 1024, "shared memory");   // (1 KB a CTA is the system's)
+    static_assert(kWarps * 32 * 16 <= kWarps * kRows * kPitchM * 4 && kOffMerge % 16 == 0, "the sequences' table");
+    static_assert((kSmem + 2048) * kCtas <= 228 * 1024, "shared memory");   // (of 228 KB; 1 KB a CTA is the system's, 1 KB static)
 };
 // (not volatile: the compiler may move products apart whose sums wait for one another)
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -126,9 +127,9 @@ __device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c, int limi
     c.each = c.len == 0 ? 1 : (c.nb + kFixed > limit ? 0 : c.nb + kFixed);
 }
 __device__ __forceinline__ int head_cost(const AttnArgs &a, const Job &c) { return c.valid * c.each + a.chunks - c.valid; }
-__device__ __forceinline__ int pieces_of(const Job &c, int limit)   // of a reading job that is cut
+__device__ __forceinline__ int pieces_of(int nb, int limit)   // of a reading job that is cut
 {
-    return max(1, min((int)ceilf(__fdividef((float)c.nb, (float)(limit - kFixed - kMeeting))), c.nb / kWarps));
+    return max(1, min((int)ceilf(__fdividef((float)nb, (float)(limit - kFixed - kMeeting))), nb / kWarps));
 }
 template <int ROWS>
 __device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int limit)   // the next one that counts
@@ -172,23 +173,28 @@ __global__ void __launch_bounds__(128) kv4_features_kernel(const __grid_constant
     uint32_t u[W32];
 #pragma unroll
     for (int i = 0; i < W32; ++i) u[i] = sel::key_image((float)e[i]);
-    uint32_t tau = 0;   // largest value that at least kd keys reach
+    // Largest value that at least kd keys reach, two bits a turn: three counts side by side in a word.  (Sums by shuffles: a reduction
+    // instruction takes some 200 cycles.)  The square of one bf16 number ends eight bits higher.
+    auto total = [](int n) {
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+        return n;
+    };
+    uint32_t tau = 0;
 #pragma unroll 1
-    for (int bit = 30; bit >= 0; bit -= 2) {
-        int n[3] = {0, 0, 0};
+    for (int bit = 30; bit >= (rows == 1 ? 8 : 0); bit -= 2) {
+        int n = 0;
 #pragma unroll
         for (int i = 0; i < W32; ++i)
 #pragma unroll
-            for (int v = 0; v < 3; ++v) n[v] += u[i] >= (tau | ((unsigned)(v + 1) << bit)) ? 1 : 0;
-        unsigned digit = 0;
-#pragma unroll
-        for (int v = 0; v < 3; ++v) digit += __reduce_add_sync(0xffffffffu, n[v]) >= a.kd ? 1u : 0u;
-        tau |= digit << bit;
+            for (int v = 0; v < 3; ++v) n += u[i] >= (tau | ((unsigned)(v + 1) << bit)) ? 1 << (10 * v) : 0;
+        n = total(n);
+        tau |= (unsigned)((n & 1023) >= a.kd) + (unsigned)((n >> 10 & 1023) >= a.kd) + (unsigned)((n >> 20) >= a.kd) << bit;
     }
     int n = 0;
 #pragma unroll
     for (int i = 0; i < W32; ++i) n += u[i] > tau ? 1 : 0;
-    int need = a.kd - __reduce_add_sync(0xffffffffu, n), at = 0;
+    int need = a.kd - total(n), at = 0;
     int32_t *out = idx_feat != nullptr && rows > 0 ? idx_feat + job * a.kd : nullptr;
 #pragma unroll
     for (int i = 0; i < W32; ++i) {
@@ -210,7 +216,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32, THREADS = kWarps * 32;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ Job s_cur, s_pc[kWarps];   // the job at hand, and the one that a warp asks for (kept out of the registers of the loop over the keys)
-    __shared__ int s_need[kLimits][kWarps], s_scan[2][kWarps], s_begin[2], abort_flag, s_last;
+    __shared__ float s_need[kLimits][kWarps];
+    __shared__ int s_scan[2][kWarps], s_begin[2], abort_flag, s_last;
     int64_t *row_out = reinterpret_cast<int64_t *>(smem + S::kOffOut);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * ST * S::kPairBytes, bars = smem_u32(smem) + S::kOffBar + warp * ST * 8;
@@ -219,6 +226,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     float *merge = reinterpret_cast<float *>(smem + S::kOffMerge), *ml = reinterpret_cast<float *>(smem + S::kOffMl);
     float *row_scale = reinterpret_cast<float *>(smem + S::kOffRow), *row_sum = row_scale + 2 * ROWS, *tot = reinterpret_cast<float *>(smem + S::kOffTot);
     int *row_vis = reinterpret_cast<int *>(row_scale + ROWS);
+    int4 *s_seq = reinterpret_cast<int4 *>(merge);   // (before there is anything to merge)
 
     if (lane == 0)
         for (int i = 0; i < ST; ++i) mbar_init(bars + 8 * i, 1);
@@ -229,55 +237,51 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
 
     // ---- this CTA's share
     Job cur;
-    int total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-        int v = 0;
+    int total = 0;   // (less than 2^31: the host sees to that)
+    auto look = [&](int b0) {   // (reading job's cost, its pairs, row tiles that hold rows) of this thread's sequence
         cur.b = b0 + tid;
-        if (cur.b < a.B) {
-            job_sequence<ROWS>(a, cur, INT32_MAX);
-            v = a.Hkv * head_cost(a, cur);
-        }
-        v = __reduce_add_sync(0xffffffffu, v);
+        if (cur.b < a.B) job_sequence<ROWS>(a, cur, INT32_MAX);
+        s_seq[tid] = cur.b < a.B ? make_int4(cur.len > 0 ? cur.each : 0, cur.nb, cur.valid, head_cost(a, cur)) : make_int4(0, 0, 0, 0);
+    };
+    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         if (b0 > 0) __syncthreads();
+        look(b0);
+        const int v = __reduce_add_sync(0xffffffffu, s_seq[tid].w);
         if (lane == 0) s_scan[0][warp] = v;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) total += s_scan[0][w];
     }
+    total *= a.Hkv;
     const int share = max(kLeast, (total + (int)gridDim.x - 1) / (int)gridDim.x);
     int limit = share;
     {
-        int need[kLimits];   // CTAs that a limit asks for, in 64ths (many more than there are: 2^14 of them)
-#pragma unroll
-        for (int k = 0; k < kLimits; ++k) need[k] = 0;
+        // CTAs that a limit asks for, a limit a lane of eight
+        const int t = share * kLimit[tid % kLimits] / 16;
+        float need = 0.f;
         for (int b0 = 0; b0 < a.B; b0 += THREADS) {
             if (a.B > THREADS) {
-                cur.b = b0 + tid;
-                if (cur.b < a.B) job_sequence<ROWS>(a, cur, INT32_MAX);
+                __syncthreads();
+                look(b0);
+                __syncthreads();
             }
-            if (cur.b < a.B) {
-#pragma unroll
-                for (int k = 0; k < kLimits; ++k) {
-                    const int t = share * kLimit[k] / 16;
-                    const bool cut = cur.len > 0 && cur.each > t;
-                    const float ctas = cut ? (float)cur.valid * (float)pieces_of(cur, t) : 0.f;
-                    const float rest = (float)(cut ? a.chunks - cur.valid : head_cost(a, cur));
-                    need[k] = min(need[k] + (int)fminf(ceilf(64.f * (float)a.Hkv * (ctas + __fdividef(rest, (float)t))), 1048576.f), 1048576);
-                }
+            for (int i = tid / kLimits; i < min(THREADS, a.B - b0); i += THREADS / kLimits) {
+                const int4 q = s_seq[i];
+                const bool cut = q.x > t;
+                const float rest = (float)(cut ? a.chunks - q.z : q.w);
+                need += (cut ? (float)q.z * (float)pieces_of(q.y, t) : 0.f) + __fdividef(rest, (float)t);
             }
         }
 #pragma unroll
-        for (int k = 0; k < kLimits; ++k) {
-            const int v = warp * 32 < a.B ? __reduce_add_sync(0xffffffffu, need[k]) : 0;
-            if (lane == 0) s_need[k][warp] = v;
-        }
+        for (int d = kLimits; d < 32; d <<= 1) need += __shfl_xor_sync(0xffffffffu, need, d);
+        if (lane < kLimits) s_need[lane][warp] = need;
         __syncthreads();
 #pragma unroll
         for (int k = kLimits - 1; k >= 0; --k) {
-            int v = 0;
+            float v = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) v += s_need[k][w];
-            if (k == kLimits - 1 || v <= 64 * (int)gridDim.x) limit = share * kLimit[k] / 16;
+            if (k == kLimits - 1 || v * (float)a.Hkv <= (float)gridDim.x - 0.01f) limit = share * kLimit[k] / 16;
         }
     }
     // CTAs with a piece of a job, and what the other jobs count: this thread's sequence, the sequences up to it, all
@@ -291,7 +295,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         }
         mine[0] = mine[1] = 0;
         if (cur.b < a.B) {
-            mine[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur, limit) : 0;
+            mine[0] = cur.each == 0 ? a.Hkv * cur.valid * pieces_of(cur.nb, limit) : 0;
             mine[1] = a.Hkv * head_cost(a, cur);
         }
         upto[0] = mine[0];
@@ -346,7 +350,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     cur.b = s_begin[0];
     job_sequence<ROWS>(a, cur, limit);
     if (piece) {
-        pieces = pieces_of(cur, limit);
+        pieces = pieces_of(cur.nb, limit);
         const int off = u_begin - s_begin[1], job = off / pieces, k = off - job * pieces, nb = cur.nb / pieces, more = cur.nb - nb * pieces;
         piece0 = (int)blockIdx.x - k;
         cur.hk = job / cur.valid;
