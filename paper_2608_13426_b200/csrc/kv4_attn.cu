@@ -62,8 +62,8 @@ struct AttnArgs {
 template <int D, int NT>
 struct Shape {
     static constexpr int kRows = 8 * NT, kBlockBytes = 18 * D, kPairBytes = 2 * kBlockBytes, kGroups = D / 64;
-    static constexpr int kCtas = D * NT <= 128 ? 4 : 2;                        // an SM
-    static constexpr int kStages = D == 64 ? (NT == 1 ? 4 : 3) : (D == 128 && NT == 2 ? 4 : 2);
+    static constexpr int kCtas = D * NT <= 128 ? 3 : 2;                        // an SM (two, three and four of heads of 128: 45.1, 42.7, 44.5 us)
+    static constexpr int kStages = D == 64 ? (NT == 1 ? 6 : 4) : (D == 128 ? (NT == 1 ? 3 : 4) : 2);
     static constexpr int kPitchM = 68, kPitchP = D + 4;                        // of a row in the merge and among the parts
     static constexpr int kOffQ = kWarps * kStages * kPairBytes;                // fp16 fragments [row tile of 8][D / 32][lane][4 words]
     static constexpr int kOffMerge = kOffQ + kRows * D * 2;                    // fp32 [warp][row][pitch]

@@ -18,8 +18,8 @@ struct CacheArgs {
     HeadRows k, v;
     kv4::View cache;
     RopeView rope;
-    int64_t groups;             // groups of neighbouring tokens of one sequence, per sequence
-    int64_t B, L;
+    int groups, units;             // groups of neighbouring tokens of one sequence: per sequence, in all
+    int64_t L;
     int heads_each, head_groups;   // heads of a warp
     int *status;
 };
@@ -49,7 +49,8 @@ __device__ __forceinline__ void quantise8(const uint32_t (&w)[4], Eight &n, floa
     for (int d = 4; d > 0; d >>= 1) ends = min_bf16x2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
     m = bf16_bits(ends);
     const float hi = -__uint_as_float(ends & 0xffff0000u);
-    s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, m), 15.f)));
+    const float range = __fsub_rn(hi, m), fifteenth = range * (1.f / 15.f);
+    s = __bfloat162float(__float2bfloat16_rn(fmaf(fmaf(-15.f, fifteenth, range), 1.f / 15.f, fifteenth)));   // (rounded as a division is)
     float r = __fdividef(1.f, s);
     r = fmaf(fmaf(-s, r, 1.f), r, r);
     const uint64_t inv = both(r), step = both(-s), least = both(-m), magic = both(12582912.f), minus = both(-12582912.f);
@@ -99,11 +100,12 @@ struct Place {
     int h0, h1, col, t;
     bool row, live;     // a row of the call; one that is a token
     uint8_t *base;      // its block of head h0, or NULL
-    __device__ __forceinline__ bool find(const CacheArgs &a, int64_t unit, int64_t table_rows)
+    __device__ __forceinline__ bool find(const CacheArgs &a, int unit, int64_t table_rows)
     {
         const int lane = threadIdx.x & 31;
-        b = unit / a.groups;
-        i = (unit - b * a.groups) * (32 / LANES) + lane / LANES;
+        const int sequence = unit / a.groups;
+        b = sequence;
+        i = (unit - sequence * a.groups) * (32 / LANES) + lane / LANES;
         col = (lane & (LANES - 1)) * 8;
         h0 = (int)(blockIdx.x % a.head_groups) * a.heads_each;
         h1 = min(a.k.heads, h0 + a.heads_each);
@@ -122,19 +124,20 @@ struct Place {
     }
 };
 
-template <typename TI, bool HELD, int LANES>
+// PLAIN: whole vectors in and out
+template <typename TI, bool HELD, bool PLAIN, int LANES>
 __global__ void __launch_bounds__(kWarps * 32, 2) kv4_append_kernel(const __grid_constant__ CacheArgs a)
 {
     constexpr int D = LANES * 8;
     pdl_wait();
-    const int64_t unit = (int64_t)(blockIdx.x / a.head_groups) * kWarps + (threadIdx.x >> 5);
-    if (unit >= a.B * a.groups) return;
+    const int unit = (int)(blockIdx.x / a.head_groups) * kWarps + (int)(threadIdx.x >> 5);
+    if (unit >= a.units) return;
     Place<LANES> p;
     const bool live = p.find(a, unit, a.rope.table != nullptr ? a.rope.rows : INT64_MAX);
     const int64_t position = live ? p.at : 0;
     const TI *ks = static_cast<const TI *>(a.k.src) + p.b * a.k.s_b + p.i * a.k.s_r + p.h0 * a.k.s_h + p.col;
     const TI *vs = static_cast<const TI *>(a.v.src) + p.b * a.v.s_b + p.i * a.v.s_r + p.h0 * a.v.s_h + p.col;
-    const bool k_vec = a.k.vec_in != 0, v_vec = a.v.vec_in != 0;
+    const bool k_vec = PLAIN || a.k.vec_in != 0, v_vec = PLAIN || a.v.vec_in != 0, k_out = PLAIN || a.k.vec_out != 0, v_out = PLAIN || a.v.vec_out != 0;
     Raw8<TI> x = zero_raw<TI>(), v = x, x_ahead = x, v_ahead = x;
     if (live) {
         x = load_raw(ks, k_vec);
@@ -190,8 +193,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv4_append_kernel(const __grid
                     nk[e] = ptx::ffma2(sk2, nk[e], mk2);
                     nv[e] = ptx::ffma2(sv2, nv[e], mv2);
                 }
-                store8(kh, a.k.vec_out != 0, nk);
-                store8(vh, a.v.vec_out != 0, nv);
+                store8(kh, k_out, nk);
+                store8(vh, v_out, nv);
             }
             kh += a.k.d_h;
             vh += a.v.d_h;
@@ -201,13 +204,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv4_append_kernel(const __grid
     }
 }
 
-template <typename TO, int LANES>
+template <typename TO, bool PLAIN, int LANES>
 __global__ void __launch_bounds__(kWarps * 32) kv4_read_kernel(const __grid_constant__ CacheArgs a)
 {
     constexpr int D = LANES * 8;
     pdl_wait();
-    const int64_t unit = (int64_t)(blockIdx.x / a.head_groups) * kWarps + (threadIdx.x >> 5);
-    if (unit >= a.B * a.groups) return;
+    const int unit = (int)(blockIdx.x / a.head_groups) * kWarps + (int)(threadIdx.x >> 5);
+    if (unit >= a.units) return;
     Place<LANES> p;
     p.find(a, unit, INT64_MAX);
     if (!p.row) return;
@@ -224,8 +227,8 @@ __global__ void __launch_bounds__(kWarps * 32) kv4_read_kernel(const __grid_cons
             dequantise8(base[value], base[pair + D / 4], v);
             base += a.cache.head_stride / 4;
         }
-        store8(kh, a.k.vec_out != 0, k);
-        store8(vh, a.v.vec_out != 0, v);
+        store8(kh, PLAIN || a.k.vec_out != 0, k);
+        store8(vh, PLAIN || a.v.vec_out != 0, v);
         kh += a.k.d_h;
         vh += a.v.d_h;
     }
@@ -236,12 +239,14 @@ int fill(CacheArgs &a, const HeadRows &K, const HeadRows &V, const kv4::View &ca
     a.k = K;
     a.v = V;
     a.cache = cache;
-    a.B = B;
     a.L = L;
-    a.groups = ceil_div(L, 256 / D);
+    const int64_t groups = ceil_div(L, 256 / D);
+    if (B * groups > INT32_MAX - kWarps) return fail(RMM_ERR_UNSUPPORTED, "kv4: more than 2^31 groups of rows");
+    a.groups = (int)groups;
+    a.units = (int)(B * groups);
     a.status = status;
     // All heads of a token by one warp, where that still leaves sixteen warps an SM
-    const int64_t token_blocks = ceil_div(B * a.groups, kWarps), want = ceil_div((int64_t)sm_count() * 2, token_blocks);
+    const int64_t token_blocks = ceil_div(a.units, kWarps), want = ceil_div((int64_t)sm_count() * 2, token_blocks);
     a.head_groups = (int)(want < K.heads ? want : K.heads);
     a.heads_each = (int)ceil_div(K.heads, a.head_groups);
     a.head_groups = (int)ceil_div(K.heads, a.heads_each);
@@ -250,15 +255,25 @@ int fill(CacheArgs &a, const HeadRows &K, const HeadRows &V, const kv4::View &ca
 }
 
 using Kernel = void (*)(CacheArgs);
-template <typename TI, bool HELD>
-Kernel append_kernel(int64_t D)
+template <typename TI, bool HELD, bool PLAIN>
+Kernel append_of(int64_t D)
 {
-    return D == 64 ? kv4_append_kernel<TI, HELD, 8> : (D == 128 ? kv4_append_kernel<TI, HELD, 16> : kv4_append_kernel<TI, HELD, 32>);
+    return D == 64 ? kv4_append_kernel<TI, HELD, PLAIN, 8> : (D == 128 ? kv4_append_kernel<TI, HELD, PLAIN, 16> : kv4_append_kernel<TI, HELD, PLAIN, 32>);
+}
+template <typename TI>
+Kernel append_kernel(int64_t D, bool held, bool plain)
+{
+    return held ? (plain ? append_of<TI, true, true>(D) : append_of<TI, true, false>(D)) : (plain ? append_of<TI, false, true>(D) : append_of<TI, false, false>(D));
+}
+template <typename TO, bool PLAIN>
+Kernel read_of(int64_t D)
+{
+    return D == 64 ? kv4_read_kernel<TO, PLAIN, 8> : (D == 128 ? kv4_read_kernel<TO, PLAIN, 16> : kv4_read_kernel<TO, PLAIN, 32>);
 }
 template <typename TO>
-Kernel read_kernel(int64_t D)
+Kernel read_kernel(int64_t D, bool plain)
 {
-    return D == 64 ? kv4_read_kernel<TO, 8> : (D == 128 ? kv4_read_kernel<TO, 16> : kv4_read_kernel<TO, 32>);
+    return plain ? read_of<TO, true>(D) : read_of<TO, false>(D);
 }
 
 }  // namespace
@@ -267,12 +282,11 @@ int launch_kv4_append(const HeadRows &K, const HeadRows &V, const kv4::View &cac
                       int *status, cudaStream_t stream)
 {
     CacheArgs a = {};
-    int64_t blocks;
+    int64_t blocks = 0;
     a.rope = rope;
     if (int rc = fill(a, K, V, cache, B, L, D, status, blocks)) return rc;
-    const bool held = K.dst != nullptr;
-    const Kernel kern = in_bf16 ? (held ? append_kernel<__nv_bfloat16, true>(D) : append_kernel<__nv_bfloat16, false>(D))
-                                : (held ? append_kernel<float, true>(D) : append_kernel<float, false>(D));
+    const bool held = K.dst != nullptr, plain = K.vec_in && V.vec_in && (!held || (K.vec_out && V.vec_out));
+    const Kernel kern = in_bf16 ? append_kernel<__nv_bfloat16>(D, held, plain) : append_kernel<float>(D, held, plain);
     prof_begin("kv4_append_kernel", stream);
     launch_kernel(kern, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, a);
     return check_launch("kv4_append_kernel", stream);
@@ -282,9 +296,10 @@ int launch_kv4_read(const HeadRows &K, const HeadRows &V, const kv4::View &cache
                     cudaStream_t stream)
 {
     CacheArgs a = {};
-    int64_t blocks;
+    int64_t blocks = 0;
     if (int rc = fill(a, K, V, cache, B, L, D, status, blocks)) return rc;
-    const Kernel kern = out_bf16 ? read_kernel<__nv_bfloat16>(D) : read_kernel<float>(D);
+    const bool plain = K.vec_out && V.vec_out;
+    const Kernel kern = out_bf16 ? read_kernel<__nv_bfloat16>(D, plain) : read_kernel<float>(D, plain);
     prof_begin("kv4_read_kernel", stream);
     launch_kernel(kern, dim3((unsigned)blocks), dim3(kWarps * 32), 0, stream, 1, a);
     return check_launch("kv4_read_kernel", stream);

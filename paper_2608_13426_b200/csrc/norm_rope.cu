@@ -4,6 +4,8 @@
 // Bound: HBM, each head read and written once.  A row's columns sit in neighbouring lanes, eight each (16 bytes of bf16), so a
 // row never leaves its lanes: squares meet by shuffles, pairs are exchanged by shuffles.  A warp takes one token and several heads: its
 // cosines, sines and weights are read once and stay in registers (a table's row is as large as two heads).
+#include <type_traits>
+
 #include "heads.cuh"
 
 namespace rmm {
@@ -14,8 +16,8 @@ constexpr int kWarps = 8;   // of a block: neighbouring tokens
 struct NormRopeArgs {
     HeadRows rows[2];
     RopeView rope;
-    int64_t tokens, L;
-    int D, rounds, groups[2];   // kTurns rows a lane, so many times; warps that share a token's heads
+    int tokens, L, D;
+    int rounds, groups[2];   // kTurns rows a lane, so many times; warps that share a token's heads
     float inv_d;
     int *status;
 };
@@ -29,12 +31,11 @@ __global__ void __launch_bounds__(kWarps * 32, 3) norm_rope_kernel(const __grid_
     constexpr int T = kTurns<TI>, PER = 32 / LANES;
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int all = a.groups[0] + a.groups[1], g = blockIdx.x % all;
-    const int64_t token = (int64_t)(blockIdx.x / all) * kWarps + warp;
+    const int all = a.groups[0] + a.groups[1], block = blockIdx.x / all, g = blockIdx.x - block * all, token = block * kWarps + warp;
     if (token >= a.tokens) return;
     const bool second = g >= a.groups[0];
     const HeadRows &h = a.rows[second];
-    const int64_t b = token / a.L, i = token - b * a.L;
+    const int b = token / a.L, i = token - b * a.L;
     const int first = (second ? g - a.groups[0] : g) * PER * T * a.rounds, mine = first + lane / LANES, col = (lane & (LANES - 1)) * 8;
     const int end = min(h.heads, first + PER * T * a.rounds);
     const int64_t position = a.rope.positions != nullptr ? a.rope.positions[b * a.rope.p_b + i * a.rope.p_r] : i;
@@ -42,33 +43,40 @@ __global__ void __launch_bounds__(kWarps * 32, 3) norm_rope_kernel(const __grid_
         if (lane == 0) atomicExch(a.status, (int)RMM_ERR_BOUNDS);
         return;
     }
-    const bool in_row = col < a.D, vec_in = h.vec_in != 0, vec_out = h.vec_out != 0;
     const int64_t s_step = PER * h.s_h, d_step = PER * h.d_h;
     const TI *src = static_cast<const TI *>(h.src) + b * h.s_b + i * h.s_r + mine * h.s_h + col;
     TO *dst = static_cast<TO *>(h.dst) + b * h.d_b + i * h.d_r + mine * h.d_h + col;
-    Raw8<TI> x[T], ahead[T];
-    auto load = [&](int head0, Raw8<TI> (&to)[T]) {
+    // PLAIN: whole vectors in and out
+    auto rows = [&](auto plain) {
+        constexpr bool PLAIN = decltype(plain)::value;
+        const bool in_row = col < a.D, vec_in = PLAIN || h.vec_in != 0, vec_out = PLAIN || h.vec_out != 0;
+        Raw8<TI> x[T], ahead[T];
+        auto load = [&](int head0, Raw8<TI> (&to)[T]) {
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            to[t] = head0 + t * PER < end && in_row ? load_raw(src, vec_in) : zero_raw<TI>();
-            src += s_step;
+            for (int t = 0; t < T; ++t) {
+                to[t] = zero_raw<TI>();
+                if (head0 + t * PER < end && in_row) to[t] = load_raw(src, vec_in);
+                src += s_step;
+            }
+        };
+        load(mine, x);
+        RowLane k;
+        row_lane(k, h.weight, a.rope, position, col, a.D);
+        for (int head0 = first; head0 < end; head0 += PER * T) {
+            load(head0 + lane / LANES + PER * T, ahead);
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                Eight z;
+                norm_rope_row<LANES>(x[t], k, a.inv_d, a.rope.eps, z);
+                if (head0 + lane / LANES + t * PER < end && in_row) store8(dst, vec_out, z);
+                dst += d_step;
+            }
+#pragma unroll
+            for (int t = 0; t < T; ++t) x[t] = ahead[t];
         }
     };
-    load(mine, x);
-    RowLane k;
-    row_lane(k, h.weight, a.rope, position, col, a.D);
-    for (int head0 = first; head0 < end; head0 += PER * T) {
-        load(head0 + lane / LANES + PER * T, ahead);
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-            Eight z;
-            norm_rope_row<LANES>(x[t], k, a.inv_d, a.rope.eps, z);
-            if (head0 + lane / LANES + t * PER < end && in_row) store8(dst, vec_out, z);
-            dst += d_step;
-        }
-#pragma unroll
-        for (int t = 0; t < T; ++t) x[t] = ahead[t];
-    }
+    if (h.vec_in != 0 && h.vec_out != 0) rows(std::true_type{});
+    else rows(std::false_type{});
 }
 
 template <typename TI, typename TO>
@@ -94,8 +102,9 @@ int launch_norm_rope(const HeadRows (&rows)[2], int in_bf16, int out_bf16, const
     a.rows[0] = rows[0];
     a.rows[1] = rows[1];
     a.rope = rope;
-    a.tokens = B * L;
-    a.L = L;
+    if (B * L > INT32_MAX - kWarps) return fail(RMM_ERR_UNSUPPORTED, "qk_norm_rope: more than 2^31 tokens");
+    a.tokens = (int)(B * L);
+    a.L = (int)L;
     a.D = (int)D;
     a.inv_d = 1.f / (float)D;
     a.status = status;
@@ -105,7 +114,7 @@ int launch_norm_rope(const HeadRows (&rows)[2], int in_bf16, int out_bf16, const
     // A warp takes up to four times as many heads of its token as it asks for at once, as long as that leaves sixteen warps an SM
     const int64_t most = rows[0].heads > rows[1].heads ? rows[0].heads : rows[1].heads;
     for (a.rounds = 4; a.rounds > 1; a.rounds /= 2)
-        if (at_once * (a.rounds / 2) < most && a.tokens * ceil_div(most, at_once * a.rounds) >= (int64_t)sm_count() * 16) break;
+        if (at_once * (a.rounds / 2) < most && (int64_t)a.tokens * ceil_div(most, at_once * a.rounds) >= (int64_t)sm_count() * 16) break;
     for (int i = 0; i < 2; ++i) a.groups[i] = (int)ceil_div(rows[i].heads, at_once * a.rounds);
     const int64_t blocks = ceil_div(a.tokens, kWarps) * (a.groups[0] + a.groups[1]);
     if (blocks > INT32_MAX) return fail(RMM_ERR_UNSUPPORTED, "qk_norm_rope: more than 2^31 blocks of rows");
