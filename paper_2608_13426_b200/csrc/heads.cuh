@@ -218,9 +218,9 @@ __device__ __forceinline__ void row_lane(RowLane &k, const void *weight, const R
     }
 }
 
-// x, x' of a row and what its norm scales with.  All lanes of the warp take part; lanes past the row's columns hold zeros.
+// x, x' of a row, and its mean square with eps.  All lanes of the warp take part; lanes past the row's columns hold zeros.
 template <int LANES, typename T>
-__device__ __forceinline__ float row_scale(const Raw8<T> &raw, const RowLane &k, float inv_d, float eps, Eight &x, Eight &xp)
+__device__ __forceinline__ float row_square(const Raw8<T> &raw, const RowLane &k, float inv_d, float eps, Eight &x, Eight &xp)
 {
     widen(raw, x);
     if (k.self) {
@@ -241,7 +241,7 @@ __device__ __forceinline__ float row_scale(const Raw8<T> &raw, const RowLane &k,
     sum += hi;
 #pragma unroll
     for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    return rsqrtf(fmaf(sum, inv_d, eps));
+    return fmaf(sum, inv_d, eps);
 }
 
 // A row in fp32.
@@ -249,49 +249,51 @@ template <int LANES, typename T>
 __device__ __forceinline__ void norm_rope_row(const Raw8<T> &raw, const RowLane &k, float inv_d, float eps, Eight &z)
 {
     Eight x, xp;
-    const uint64_t r = both(row_scale<LANES>(raw, k, inv_d, eps, x, xp));
+    const float v = row_square<LANES>(raw, k, inv_d, eps, x, xp);
+    const uint64_t r = both(k.norm ? rsqrtf(v) : 1.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) z[i] = fmul2(ptx::ffma2(x[i], k.a[i], fmul2(xp[i], k.b[i])), r);
 }
 
-// The same row in 64 bits, rounded once to bf16.  (Out of the way: few rows come here.)
+// What a row's norm scales with, in 64 bits.  (Out of the way, as the next: few rows come here.)
 template <int LANES>
-__device__ __noinline__ void norm_rope_row_64(const Eight &x2, const Eight &xp2, uint32_t *out, const void *weight, const RopeView &r, int64_t position, int col)
+__device__ __noinline__ double row_scale_64(uint64_t x0, uint64_t x1, uint64_t x2, uint64_t x3, float eps)
 {
-    constexpr int D = LANES * 8;
-    float x[8], xp[8], z[8];
+    const Eight x2s = {x0, x1, x2, x3};
+    double sum = 0.0;
     for (int i = 0; i < 4; ++i) {
-        ptx::unpack2(x2[i], x[2 * i], x[2 * i + 1]);
-        ptx::unpack2(xp2[i], xp[2 * i], xp[2 * i + 1]);
+        float a, b;
+        ptx::unpack2(x2s[i], a, b);
+        sum = fma((double)b, (double)b, fma((double)a, (double)a, sum));
     }
-    double sum = 0.0, w = 1.0;
-    for (int i = 0; i < 8; ++i) sum = fma((double)x[i], (double)x[i], sum);
     for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (weight != nullptr) w = 1.0 / sqrt(sum / (double)D + (double)r.eps);
-    const int chunk = col / 8, other = row_partner(r, chunk);
-    const bool turns = chunk < r.rot / 8;
-    float c[8], s[8];
-    if (turns) row_angles(r, position, col, c, s);
-    auto weight_of = [&](int d) -> double {
+    return 1.0 / sqrt(sum / (8.0 * LANES) + (double)eps);
+}
+// Column d of a row in 64 bits, rounded once to bf16; x and x' are its own and the one it is turned against.
+static __device__ __noinline__ uint32_t element_64(float x, float xp, double r, const void *weight, const RopeView &rope, int64_t position, int d)
+{
+    const int half = rope.rot / 2;
+    const bool first = rope.interleaved ? (d & 1) == 0 : d < half;
+    auto weight_of = [&](int c) -> double {
         if (weight == nullptr) return 1.0;
-        return r.weight_bf16 ? (double)__bfloat162float(static_cast<const __nv_bfloat16 *>(weight)[d]) : (double)static_cast<const float *>(weight)[d];
+        return rope.weight_bf16 ? (double)__bfloat162float(static_cast<const __nv_bfloat16 *>(weight)[c]) : (double)static_cast<const float *>(weight)[c];
     };
-    for (int i = 0; i < 8; ++i) {
-        const double y = (double)x[i] * w * weight_of(col + i);
-        if (!turns) {
-            z[i] = bf16_of_double(y);
-            continue;
-        }
-        const double yp = (double)xp[i] * w * weight_of(r.interleaved ? col + (i ^ 1) : 8 * other + i);
-        z[i] = bf16_of_double(fma(y, (double)c[i], yp * (double)s[i]));
+    double z = (double)x * r * weight_of(d);
+    if (d < rope.rot) {
+        const int other = rope.interleaved ? d ^ 1 : (first ? d + half : d - half), at = rope.interleaved ? d / 2 : (first ? d : other);
+        const float *row = rope.table + position * rope.stride;
+        const double zp = (double)xp * r * weight_of(other), s = (double)row[half + at];
+        z = fma(z, (double)row[at], first ? -zp * s : zp * s);
     }
-    for (int i = 0; i < 4; ++i) out[i] = pack_bf16(z[2 * i], z[2 * i + 1]);
+    return __float_as_uint(bf16_of_double(z)) >> 16;
 }
 
-// A whole row (D = 8 LANES) rounded to bf16 as the 64-bit result would be.  The fp32 chain is off by at most
-// e = 2^-20 r (|x a| + |x' b|): sum of up to 256 squares in 4-element chains and 6 meetings, mean and eps (13 roundings of 2^-24, half
-// of that after the root), rsqrtf (4), a and b, two products, the scaling (4).  Where z - e and z + e round to different numbers, in one
-// row of 20 or so, the warp's rows are done again in 64 bits.
+// A whole row (D = 8 LANES) rounded to bf16 as the 64-bit result would be.  With u = 2^-24 the fp32 chain is off by at most
+// r (10 u |x a| + 11 u |x' b|): a sum of up to 256 squares in chains of four, one sum of two and up to five meetings, mean and eps (11
+// roundings, of which the root halves the effect), rsqrtf after one step of Newton's (1), a and b (1), two products (2), the scaling (1);
+// e is 12 u.  A column where z - e and z + e round to different numbers, one of 1500 or so, is done again in 64 bits; so is a row whose
+// squares leave the range of fp32.  (4 x 4096 tokens, 8 heads of 128 appended in 44 us; in 62 where such a
+// column's whole row was done again.)
 template <int LANES, typename T>
 __device__ __forceinline__ void norm_rope_row_bf16(const Raw8<T> &raw, const RowLane &k, const void *weight, const RopeView &rope, int64_t position,
                                                    int col, uint32_t (&out)[4])
@@ -304,9 +306,16 @@ __device__ __forceinline__ void norm_rope_row_bf16(const Raw8<T> &raw, const Row
         return;
     }
     Eight x, xp;
-    const float r = row_scale<LANES>(raw, k, 1.f / (8 * LANES), rope.eps, x, xp), er = r * 9.5367431640625e-7f;
+    const float v = row_square<LANES>(raw, k, 1.f / (8 * LANES), rope.eps, x, xp);
+    float r = 1.f, er = 4 * 5.9604645e-8f;   // (a rotation alone: a product and a sum)
+    if (k.norm) {
+        r = rsqrtf(v);
+        r = fmaf(0.5f * r, fmaf(-(v * r), r, 1.f), r);
+        er = r * (12 * 5.9604645e-8f);
+    }
     const uint64_t r2 = both(r);
-    uint32_t differ = 0;
+    const bool range = v > 1e-30f && v < 1e37f;
+    uint32_t differ[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint64_t t = fmul2(xp[i], k.b[i]), z = fmul2(ptx::ffma2(x[i], k.a[i], t), r2);
@@ -317,10 +326,21 @@ __device__ __forceinline__ void norm_rope_row_bf16(const Raw8<T> &raw, const Row
         ptx::unpack2(z, z0, z1);
         const float s0 = fmaf(fabsf(x0), fabsf(a0), fabsf(t0)), s1 = fmaf(fabsf(x1), fabsf(a1), fabsf(t1));
         out[i] = pack_bf16(fmaf(s0, er, z0), fmaf(s1, er, z1));
-        differ |= out[i] ^ pack_bf16(fmaf(s0, -er, z0), fmaf(s1, -er, z1));
+        differ[i] = out[i] ^ pack_bf16(fmaf(s0, -er, z0), fmaf(s1, -er, z1));
     }
     // (a sign's difference alone is a zero's)
-    if (__any_sync(0xffffffffu, differ != 0)) norm_rope_row_64<LANES>(x, xp, out, weight, rope, position, col);
+    if (__any_sync(0xffffffffu, ((differ[0] | differ[1]) | (differ[2] | differ[3])) != 0 || !range)) {
+        double r64 = 1.0;
+        if (k.norm) r64 = row_scale_64<LANES>(x[0], x[1], x[2], x[3], rope.eps);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x0, x1, p0, p1;
+            ptx::unpack2(x[i], x0, x1);
+            ptx::unpack2(xp[i], p0, p1);
+            if ((differ[i] & 0xffffu) != 0 || !range) out[i] = __byte_perm(out[i], element_64(x0, p0, r64, weight, rope, position, col + 2 * i), 0x3254);
+            if ((differ[i] >> 16) != 0 || !range) out[i] = __byte_perm(out[i], element_64(x1, p1, r64, weight, rope, position, col + 2 * i + 1), 0x5410);
+        }
+    }
 }
 
 int launch_norm_rope(const HeadRows (&rows)[2], int in_bf16, int out_bf16, const RopeView &rope, int64_t B, int64_t L, int64_t D, int *status,
