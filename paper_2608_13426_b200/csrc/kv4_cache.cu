@@ -12,7 +12,7 @@
 namespace rmm {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 
 struct CacheArgs {
     HeadRows k, v;
@@ -124,9 +124,10 @@ struct Place {
     }
 };
 
-// PLAIN: whole vectors in and out
+// PLAIN: whole vectors in and out.  (Blocks an SM: the next head's rows in fp32 take more registers.  Five and four, 4 x 4096 tokens of 8
+// heads of 128, bf16: 37.7 and 41.3 us; 7 x 999 of 2 heads of 256, fp32: 16.3 and 15.5)
 template <typename TI, bool HELD, bool PLAIN, int LANES>
-__global__ void __launch_bounds__(kWarps * 32, 2) kv4_append_kernel(const __grid_constant__ CacheArgs a)
+__global__ void __launch_bounds__(kWarps * 32, sizeof(TI) == 2 ? 5 : 4) kv4_append_kernel(const __grid_constant__ CacheArgs a)
 {
     constexpr int D = LANES * 8;
     pdl_wait();
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv4_read_kernel(const __grid_cons
     const int key = kv4::key_word(D, p.t, chunk), value = kv4::value_word(D, p.t, chunk), pair = kv4::key_pair_word(D, p.t, chunk >> 3);
     TO *kh = static_cast<TO *>(a.k.dst) + p.b * a.k.d_b + p.i * a.k.d_r + p.h0 * a.k.d_h + p.col;
     TO *vh = static_cast<TO *>(a.v.dst) + p.b * a.v.d_b + p.i * a.v.d_r + p.h0 * a.v.d_h + p.col;
-#pragma unroll 4
+#pragma unroll 2
     for (int h = p.h0; h < p.h1; ++h) {
         Eight k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
         if (base != nullptr) {
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv4_read_kernel(const __grid_cons
     }
 }
 
-int fill(CacheArgs &a, const HeadRows &K, const HeadRows &V, const kv4::View &cache, int64_t B, int64_t L, int64_t D, int *status, int64_t &blocks)
+int fill(CacheArgs &a, const HeadRows &K, const HeadRows &V, const kv4::View &cache, int64_t B, int64_t L, int64_t D, int warps, int *status, int64_t &blocks)
 {
     a.k = K;
     a.v = V;
@@ -245,8 +246,8 @@ int fill(CacheArgs &a, const HeadRows &K, const HeadRows &V, const kv4::View &ca
     a.groups = (int)groups;
     a.units = (int)(B * groups);
     a.status = status;
-    // All heads of a token by one warp, where that still leaves sixteen warps an SM
-    const int64_t token_blocks = ceil_div(a.units, kWarps), want = ceil_div((int64_t)sm_count() * 2, token_blocks);
+    // All heads of a token by one warp, where that still leaves `warps` of them for an SM
+    const int64_t token_blocks = ceil_div(a.units, kWarps), want = ceil_div((int64_t)sm_count() * (warps / kWarps), token_blocks);
     a.head_groups = (int)(want < K.heads ? want : K.heads);
     a.heads_each = (int)ceil_div(K.heads, a.head_groups);
     a.head_groups = (int)ceil_div(K.heads, a.heads_each);
@@ -284,7 +285,9 @@ int launch_kv4_append(const HeadRows &K, const HeadRows &V, const kv4::View &cac
     CacheArgs a = {};
     int64_t blocks = 0;
     a.rope = rope;
-    if (int rc = fill(a, K, V, cache, B, L, D, status, blocks)) return rc;
+    // (a warp's angles and weights are worth some heads: 16 warps an SM append 4 x 4096 tokens of 8 heads of 128 in 37.7 us, 64 in 40.3;
+    // 7 x 999 of 2 heads of 256, fp32, in 16.3 and 19.5)
+    if (int rc = fill(a, K, V, cache, B, L, D, 16, status, blocks)) return rc;
     const bool held = K.dst != nullptr, plain = K.vec_in && V.vec_in && (!held || (K.vec_out && V.vec_out));
     const Kernel kern = in_bf16 ? append_kernel<__nv_bfloat16>(D, held, plain) : append_kernel<float>(D, held, plain);
     prof_begin("kv4_append_kernel", stream);
@@ -297,7 +300,9 @@ int launch_kv4_read(const HeadRows &K, const HeadRows &V, const kv4::View &cache
 {
     CacheArgs a = {};
     int64_t blocks = 0;
-    if (int rc = fill(a, K, V, cache, B, L, D, status, blocks)) return rc;
+    // (a warp has little to prepare: 16 warps an SM read 7 x 362 tokens of 8 heads of 256 to fp32 in 24.4 us, 64 in 12.4; 4 x 4096 of 8
+    // heads of 128 in 18.8 and 18.1)
+    if (int rc = fill(a, K, V, cache, B, L, D, 64, status, blocks)) return rc;
     const bool plain = K.vec_out && V.vec_out;
     const Kernel kern = out_bf16 ? read_kernel<__nv_bfloat16>(D, plain) : read_kernel<float>(D, plain);
     prof_begin("kv4_read_kernel", stream);
