@@ -265,8 +265,9 @@ typedef struct {
 /* Q' = rotation(norm(Q)), K' = rotation(norm(K)) for every head's row in one pass:  y = x w / sqrt(mean x^2 + eps) with one weight
  * [D] for all query heads and one for all key heads (contiguous; NULL: that side is not normalised), then
  * (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin) for each pair.  Taken in fp32, rounded once.  D is a multiple of 8, at most
- * 256.  Q_out and K_out have the shapes of Q and K, bf16 or fp32 (both the same), and may be the inputs themselves.  K, K_out NULL:
- * queries only.  A row whose position is outside the table is not written and reported as RMM_ERR_BOUNDS.
+ * 256.  Q_out and K_out have the shapes of Q and K, bf16 or fp32 (both the same).  They may be the inputs themselves (of their dtype and
+ * strides), but overlap neither each other nor, otherwise, the inputs.  K, K_out NULL: queries only.  A row whose position is outside
+ * the table is not written and reported as RMM_ERR_BOUNDS.
  * The workspace is only used for the status word: RMM_WS_HEADER_BYTES. */
 int rmm_qk_norm_rope(const rmm_heads_t *Q, const rmm_heads_t *K, const void *q_weight, const void *k_weight, const rmm_rope_t *rope,
                      const rmm_heads_t *Q_out, const rmm_heads_t *K_out, void *ws, size_t ws_bytes, void *stream);
@@ -308,7 +309,7 @@ int rmm_kv4_read(const rmm_kv4_t *cache, const rmm_heads_t *K, const rmm_heads_t
  * no token, and the rows behind new_len[b], are zeros.  rho_d < 1 keeps ceil(rho_d Dh) features of each query head, chosen from
  * its new_len[b] rows, of which there may be 16 at most (L <= 16); idx_feat int32 [B,Hq,kd] (or NULL) receives them (not for
  * sequences without rows).  Any L is taken, 8 or 16 query rows of a kv head at a time, so that a long chunk reads the cache many times over:
- * from some 64 rows on rmm_kv4_read and rmm_reduced_attn are faster.  Softmax weights times a value's step are rounded to fp16; logits,
+ * past 128 rows or so rmm_kv4_read and rmm_reduced_attn are faster.  Softmax weights times a value's step are rounded to fp16; logits,
  * sums and O are fp32.  Inputs are finite, cached steps between 2^-80 and 2^60. */
 size_t rmm_kv4_attn_workspace_bytes(const rmm_heads_t *Q, const rmm_kv4_t *cache);
 int rmm_kv4_attn(const rmm_heads_t *Q, const rmm_kv4_t *cache, int causal, double rho_d, const rmm_heads_t *O, int32_t *idx_feat,

@@ -695,7 +695,7 @@ def rmm_kv4_attn(Q: torch.Tensor, pool: torch.Tensor, pages: torch.Tensor, lengt
                  causal: bool = True, rho_d: float = 1.0, want_idx: bool = False, ws: Optional[torch.Tensor] = None):
     """Reduced attention of Q [B,Hq,L,Dh] bf16 over the paged 4-bit cache: rows i < new_len[b] (None: all L) are the last tokens of
     lengths[b]; causal rows see the tokens up to their own, the others all.  Returns O [B,Hq,L,Dh] bf16 (zeros where a row sees
-    nothing, and behind new_len), or (O, idx_feat) with want_idx.  A call that is captured into a graph needs a `ws` of its own
+    nothing, and behind new_len), or (O, idx_feat [B,Hq,ceil(rho_d Dh)]) with want_idx (not written for a sequence without rows).  A call that is captured into a graph needs a `ws` of its own
     that lives as long as the graph, as do calls that may overlap."""
     if ws is None and not want_idx and (native := _marshal or _native()) is not None:
         done = native.kv4_attn(Q, pool, pages, lengths, new_len, causal, rho_d)

@@ -24,6 +24,36 @@ int check_same(const rmm_heads_t *x, const rmm_heads_t *y, const char *who, cons
     return RMM_OK;
 }
 
+// What a call writes: no element twice (rows that another array's lie between are fine).
+int check_written(const rmm_heads_t *x, const char *who, const char *name)
+{
+    int64_t n[3] = {x->B, x->H, x->L}, s[3] = {x->stride[0], x->stride[1], x->stride[2]}, extent = x->D;
+    for (int i = 0; i < 3; ++i) {
+        for (int j = i + 1; j < 3; ++j)   // the smallest stride that is left
+            if (n[i] == 1 || (n[j] > 1 && s[j] < s[i])) {
+                const int64_t a = n[i], b = s[i];
+                n[i] = n[j]; s[i] = s[j];
+                n[j] = a; s[j] = b;
+            }
+        if (n[i] == 1) break;
+        if (s[i] < extent) return fail(RMM_ERR_INVALID_ARG, "%s: rows of %s overlap, and it is written", who, name);
+        extent += s[i] * (n[i] - 1);
+    }
+    return RMM_OK;
+}
+int check_apart(const rmm_heads_t *x, const rmm_heads_t *y, const char *who)
+{
+    return x->ptr == y->ptr ? fail(RMM_ERR_INVALID_ARG, "%s: both outputs are the same memory", who) : (int)RMM_OK;
+}
+
+int check_in_place(const rmm_heads_t *x, const rmm_heads_t *y, const char *who)
+{
+    if (x->ptr == y->ptr && (x->dtype != y->dtype || (x->B > 1 && x->stride[0] != y->stride[0]) || (x->H > 1 && x->stride[1] != y->stride[1]) ||
+                             (x->L > 1 && x->stride[2] != y->stride[2])))
+        return fail(RMM_ERR_INVALID_ARG, "%s: in place, dtype and strides stay", who);
+    return RMM_OK;
+}
+
 int check_rope(const rmm_rope_t *r, int64_t D, const void *weight, const char *who)
 {
     if (weight != nullptr && r == nullptr) return fail(RMM_ERR_INVALID_ARG, "%s: a norm needs a description (weight type and eps)", who);
@@ -100,7 +130,7 @@ RopeView rope_of(const rmm_rope_t *r)
     v.table = r->table;
     v.rows = r->table_rows;
     v.stride = r->table_stride;
-    v.positions = r->positions;
+    v.positions = r->table != nullptr ? r->positions : nullptr;
     v.p_b = r->pos_stride[0];
     v.p_r = r->pos_stride[1];
     v.rot = r->table != nullptr ? (int)r->rot : 0;
@@ -162,7 +192,8 @@ int rmm_qk_norm_rope(const rmm_heads_t *Q, const rmm_heads_t *K, const void *q_w
     }
     if (Q->D % 8 != 0 || Q->D > 256) return fail(RMM_ERR_UNSUPPORTED, "%s: heads have a multiple of 8 columns up to 256, not %lld", who, (long long)Q->D);
     if ((rc = check_rope(rope, Q->D, q_weight, who)) || (K != nullptr && (rc = check_rope(rope, Q->D, k_weight, who)))) return rc;
-    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who))) return rc;
+    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who)) || (rc = check_written(Q_out, who, "Q_out")) || (rc = check_in_place(Q, Q_out, who))) return rc;
+    if (K != nullptr && ((rc = check_written(K_out, who, "K_out")) || (rc = check_in_place(K, K_out, who)) || (rc = check_apart(Q_out, K_out, who)))) return rc;
     const HeadRows rows[2] = {rows_of(Q, Q_out, q_weight), rows_of(K, K_out, K != nullptr ? k_weight : nullptr)};
     return launch_norm_rope(rows, Q->dtype == RMM_BF16, Q_out->dtype == RMM_BF16, rope_of(rope), Q->B, Q->L, Q->D,
                             &static_cast<WsHeader *>(ws)->status, static_cast<cudaStream_t>(stream));
@@ -185,6 +216,7 @@ int rmm_kv4_append(const rmm_heads_t *K, const rmm_heads_t *V, const rmm_kv4_t *
         if (K_held->dtype != RMM_BF16 || V_held->dtype != RMM_BF16) return fail(RMM_ERR_UNSUPPORTED, "%s: held values are bf16", who);
     }
     if ((rc = check_rope(rope, K->D, k_weight, who)) || (rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who))) return rc;
+    if (K_held != nullptr && ((rc = check_written(K_held, who, "K_held")) || (rc = check_written(V_held, who, "V_held")) || (rc = check_apart(K_held, V_held, who)))) return rc;
     return launch_kv4_append(rows_of(K, K_held, k_weight), rows_of(V, V_held, nullptr), view_of(cache, K->L), K->dtype == RMM_BF16, rope_of(rope), K->B,
                              K->L, K->D, &static_cast<WsHeader *>(ws)->status, static_cast<cudaStream_t>(stream));
 }
@@ -197,7 +229,9 @@ int rmm_kv4_read(const rmm_kv4_t *cache, const rmm_heads_t *K, const rmm_heads_t
     if (K->dtype != V->dtype) return fail(RMM_ERR_UNSUPPORTED, "%s: K and V must share a dtype", who);
     if ((rc = check_cache(cache, K->B, who))) return rc;
     if (K->H != cache->Hkv || K->D != cache->Dh) return fail(RMM_ERR_INVALID_ARG, "%s: the cache has other heads than K", who);
-    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who))) return rc;
+    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES, who)) || (rc = check_written(K, who, "K")) || (rc = check_written(V, who, "V")) ||
+        (rc = check_apart(K, V, who)))
+        return rc;
     return launch_kv4_read(rows_of(nullptr, K, nullptr), rows_of(nullptr, V, nullptr), view_of(cache, K->L), K->dtype == RMM_BF16, K->B, K->L, K->D,
                            &static_cast<WsHeader *>(ws)->status, static_cast<cudaStream_t>(stream));
 }
@@ -219,7 +253,8 @@ int rmm_kv4_attn(const rmm_heads_t *Q, const rmm_kv4_t *cache, int causal, doubl
     if (O->dtype != RMM_BF16) return fail(RMM_ERR_UNSUPPORTED, "%s: O must be bf16", who);
     if (rmm_keep_count(rho_d, p.D, &p.kd) != RMM_OK) return fail(RMM_ERR_INVALID_ARG, "%s: rho_d = %g is outside (0, 1]", who, rho_d);
     if ((p.kd < p.D || idx_feat != nullptr) && p.L > kDecodeMaxRows) return fail(RMM_ERR_UNSUPPORTED, "%s: features are selected for up to %d rows", who, (int)kDecodeMaxRows);
-    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES + kv4_attn_workspace_bytes(p), who))) return rc;
+    if (reinterpret_cast<uintptr_t>(idx_feat) % 4 != 0) return fail(RMM_ERR_UNSUPPORTED, "%s: idx_feat is misaligned", who);
+    if ((rc = check_ws(ws, ws_bytes, RMM_WS_HEADER_BYTES + kv4_attn_workspace_bytes(p), who)) || (rc = check_written(O, who, "O"))) return rc;
     p.o = O->ptr;
     p.o_sb = O->stride[0]; p.o_sh = O->stride[1]; p.o_sr = O->stride[2];
     p.causal = causal != 0;

@@ -928,9 +928,9 @@ int launch(const AttnArgs &a, cudaStream_t stream)
 
 bool kv4_attn_fits(const Kv4AttnProblem &p, const kv4::View &cache)
 {
-    // the axis of all pairs is counted in 32 bits
+    // the axis of all pairs, and with it a number below that of the grid's blocks, is counted in 32 bits
     const double chunks = (double)ceil_div(p.Hq / p.Hkv * p.L, 8 * row_tiles(p));
-    return (double)p.B * p.Hkv * chunks * (0.5 * (double)(cache.max_pages << cache.page_shift) + 1.0 + kFixed) < 2147483647.0 && p.Hq / p.Hkv * p.L < INT32_MAX / 2 &&
+    return (double)p.B * p.Hkv * chunks * (0.5 * (double)(cache.max_pages << cache.page_shift) + 1.0 + kFixed) < 2147000000.0 && p.Hq / p.Hkv * p.L < INT32_MAX / 2 &&
            p.B * p.Hq < INT32_MAX;
 }
 

@@ -296,6 +296,31 @@ def test_pools_and_tables_of_other_strides():
     assert rmm.rmm_status_read() == 0
 
 
+@pytest.mark.parametrize("page", [16, 64])
+def test_a_pool_beyond_32_bits(page):
+    """The first and the last pages of a pool of 5 GB: page numbers times bytes pass 2^32."""
+    lengths, D, Hkv = [200, 77], 128, 2
+    size = Hkv * page // 16 * 18 * D
+    pages = 5 * (1 << 30) // size
+    need = [-(-n // page) for n in lengths]
+    table = torch.full((2, max(need)), -1, dtype=torch.int32)
+    table[0, :need[0]] = pages - 1 - torch.arange(need[0])
+    table[1, :need[1]] = torch.arange(need[1])
+    big = torch.empty(pages, Hkv, page // 16, 18 * D, dtype=torch.uint8, device="cuda")
+    big[table[0, :need[0]].long().cuda()] = 255
+    big[:need[1]] = 255
+    small, order, K, V = filled(lengths, Hkv, D, page, seed=6)
+    rmm.rmm_kv4_append(K.cuda(), V.cuda(), big, table.cuda(), ints(lengths), ints(lengths))
+    for b, n in enumerate(need):
+        assert torch.equal(big[table[b, :n].long().cuda()], small[order[b, :n].long().cuda()])
+    Q = torch.randn(2, 4, 2, D, generator=gen(1)).to(BF16).cuda()
+    assert torch.equal(rmm.rmm_kv4_attn(Q, big, table.cuda(), ints(lengths)), rmm.rmm_kv4_attn(Q, small, order.cuda(), ints(lengths)))
+    for x, y in zip(rmm.rmm_kv4_read(big, table.cuda(), ints(lengths), ints(lengths), rows=200),
+                    rmm.rmm_kv4_read(small, order.cuda(), ints(lengths), ints(lengths), rows=200)):
+        assert torch.equal(x, y)
+    assert rmm.rmm_status_read() == 0
+
+
 def test_what_lies_outside_is_reported():
     """Pages that are none of the pool's, lengths and rows beyond the table: reported, skipped, nothing else is touched."""
     lengths, D = [40, 40], 64

@@ -137,6 +137,32 @@ def test_another_stream_and_a_captured_call():
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
 
 
+def test_offsets_beyond_32_bits():
+    """Sequences, heads and rows that lie more than 2^32 bytes apart."""
+    far = (1 << 31) + 128
+    memory = torch.empty(far + 4096, dtype=BF16, device="cuda")
+    x = torch.randn(2, 2, 2, 64, generator=torch.Generator().manual_seed(3)).to(BF16)
+    t = ref.table(2, 64).cuda()
+    want = rmm.rmm_qk_norm_rope(x.cuda(), rope=t)
+    for stride in ((far, 128, 64), (128, far, 64), (128, 64, far)):
+        q = memory.as_strided((2, 2, 2, 64), stride + (1,))
+        q.copy_(x)
+        assert torch.equal(rmm.rmm_qk_norm_rope(q, rope=t), want)
+        rmm.rmm_qk_norm_rope(q, rope=t, inplace=True)
+        assert torch.equal(q, want)
+    assert rmm.rmm_status_read() == 0
+
+
+def test_written_memory_that_overlaps_is_refused():
+    x = torch.zeros(1, 2, 3, 64, dtype=BF16, device="cuda")
+    for call in (lambda: rmm.rmm_qk_norm_rope(x[:, :1].expand(1, 2, 3, 64), inplace=True), lambda: rmm.rmm_qk_norm_rope(x, x, inplace=True)):
+        with pytest.raises(binding.RmmError) as e:
+            call()
+        assert e.value.code == binding.RMM_ERR_INVALID_ARG
+    rmm.rmm_qk_norm_rope(x[:, :1].expand(1, 2, 3, 64))   # read only
+    assert rmm.rmm_status_read() == 0
+
+
 def test_refusals():
     q = torch.zeros(1, 2, 3, 64, dtype=BF16, device="cuda")
     w, t = torch.ones(64, device="cuda"), ref.table(8, 64).cuda()

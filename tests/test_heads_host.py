@@ -89,6 +89,27 @@ def test_cache_refusals(L):
     assert L.rmm_kv4_attn(heads(B=1 << 20), many, 1, 1.0, heads(B=1 << 20), None, *OK_WS, None) == ODD   # the blocks' axis passes 2^31
 
 
+def test_outputs_that_overlap_are_refused(L):
+    """An element that two rows write has no one value: an expanded output, rows that reach into the next, one array for two outputs."""
+    there = 1 << 20
+    for o in (heads(there, stride=(0, 384, 128)), heads(there, stride=(1536, 0, 128)), heads(there, stride=(1536, 384, 0)),
+              heads(there, stride=(1536, 384, 120)), heads(there, stride=(1528, 384, 128)), heads(there, stride=(128, 512, 128))):
+        assert L.rmm_qk_norm_rope(heads(), None, None, None, rope(), o, None, *OK_WS, None) == BAD
+        assert L.rmm_kv4_attn(heads(), cache(), 1, 1.0, o, None, *OK_WS, None) == BAD
+        c = cache(Hkv=4, page_stride=4 * 4 * 2304)
+        assert L.rmm_kv4_read(c, o, heads(), *OK_WS, None) == BAD and L.rmm_kv4_read(c, heads(), o, *OK_WS, None) == BAD
+        assert L.rmm_kv4_append(heads(), heads(), c, None, None, o, heads(), *OK_WS, None) == BAD
+        assert L.rmm_kv4_append(heads(), heads(), c, None, None, heads(), o, *OK_WS, None) == BAD
+    k = heads(H=2)
+    assert L.rmm_qk_norm_rope(heads(), k, None, None, rope(), heads(there), heads(there, H=2), *OK_WS, None) == BAD
+    assert L.rmm_kv4_read(cache(), k, k, *OK_WS, None) == BAD
+    assert L.rmm_kv4_append(k, k, cache(), None, None, heads(there, H=2), heads(there, H=2), *OK_WS, None) == BAD
+    # in place: another dtype, other strides
+    assert L.rmm_qk_norm_rope(heads(), None, None, None, rope(), heads(dtype=1), None, *OK_WS, None) == BAD
+    assert L.rmm_qk_norm_rope(heads(), None, None, None, rope(), heads(stride=(1536, 128, 512)), None, *OK_WS, None) == BAD
+    assert L.rmm_kv4_attn(heads(), cache(), 1, 1.0, heads(there), ctypes.c_void_p(4098), *OK_WS, None) == ODD
+
+
 def test_tensors_that_are_not_the_calls():
     q = torch.zeros(1, 2, 3, 64, dtype=torch.bfloat16)
     for f in (lambda: binding.rmm_qk_norm_rope(q), lambda: binding.rmm_qk_norm_rope(None), lambda: binding.rmm_kv4_append(q, q, None, None, None),
