@@ -38,7 +38,9 @@ constexpr int kFixed = 8, kMeeting = 6;               // pairs that a job's fixe
 constexpr int kLeast = kFixed + 2 * kMeeting;         // the least limit: two pieces take no less time than a job of that size
 constexpr int kLimits = 8;                            // limits that are tried, in sixteenths of the equal share
 __device__ constexpr int kLimit[kLimits] = {16, 17, 18, 20, 23, 26, 30, 36};
-constexpr int kMeet = 16;                             // CTAs whose parts are added up in one step
+constexpr int kMeet = 16, kLonger = 8;                // CTAs whose parts are added up in one step (or one more), and pairs that a piece may be
+                                                      // longer than the limit asks for where that saves the second step
+constexpr int kGrid = 512;                            // CTAs at most
 constexpr float kTopWeight = 16384.f, kTop = 6.f, kLeastStep = 8.2718061e-25f;   // 2^14, log2 of 2^6, 2^-80: see above; smaller steps weigh as that
 constexpr float kNone = 1e30f;                       // minus the reference of a row that has seen no key
 
@@ -129,7 +131,8 @@ __device__ __forceinline__ void job_sequence(const AttnArgs &a, Job &c, int limi
 __device__ __forceinline__ int head_cost(const AttnArgs &a, const Job &c) { return c.valid * c.each + a.chunks - c.valid; }
 __device__ __forceinline__ int pieces_of(int nb, int limit)   // of a reading job that is cut
 {
-    return max(1, min((int)ceilf(__fdividef((float)nb, (float)(limit - kFixed - kMeeting))), nb / kWarps));
+    const int most = limit - kFixed - kMeeting, p = max(1, min((int)ceilf(__fdividef((float)nb, (float)most)), nb / kWarps));
+    return p > kMeet && nb <= kMeet * (most + kLonger) ? kMeet : p;
 }
 template <int ROWS>
 __device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int limit)   // the next one that counts
@@ -843,12 +846,15 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         }
     }
 
-    // ---- a job that other CTAs work on too: whichever comes last adds the parts up, in two steps where there are more than kMeet or so
+    // ---- a job that other CTAs work on too: whichever comes last adds the parts up.  More than kMeet or so meet
+    // in two steps, by eights or sixteens first
     if (pieces > 1) {
         const int row0 = s_cur.chunk * ROWS;
         const int64_t b = s_cur.b, hk = s_cur.hk;
-        const int groups = (pieces - 2) / kMeet + 1, group = min(((int)blockIdx.x - piece0) / kMeet, groups - 1);   // (none of one CTA)
-        int first_part = piece0 + group * kMeet, parts = group == groups - 1 ? pieces - group * kMeet : kMeet, apart = 1;
+        static_assert((kGrid - 2) / kMeet + 1 <= 32, "two parts a lane");
+        const int by = pieces > kMeet + 1 && pieces <= 6 * kMeet ? kMeet / 2 : kMeet, groups = (pieces - 2) / by + 1;   // (none of one CTA)
+        const int group = min(((int)blockIdx.x - piece0) / by, groups - 1);
+        int first_part = piece0 + group * by, parts = group == groups - 1 ? pieces - group * by : by, apart = 1;
         unsigned *counter = a.counters + first_part;
         while (true) {
             if (tid == 0) {
@@ -867,20 +873,40 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                     const int cta = first_part + p * apart;
                     return a.part + ((int64_t)cta * ROWS + r) * S::kPitchP;
                 };
-                float mx = -kNone, lsum = 0.f;
-                float4 sum[NG];
+                // A lane knows two parts' references and sums; the parts come U at a time
+                const unsigned half = 0xffffu << (lane & 16);
+                const float2 none = make_float2(-kNone, 0.f);
+                const float2 ref0 = c < parts ? __ldcg(reinterpret_cast<const float2 *>(at(c) + D)) : none;
+                const float2 ref1 = c + 16 < parts ? __ldcg(reinterpret_cast<const float2 *>(at(c + 16) + D)) : none;
+                constexpr int U = NG <= 2 ? 4 : 2;
+                float4 sum[NG], v[U][NG];
 #pragma unroll
                 for (int j = 0; j < NG; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int p = 0; p < parts; ++p) mx = fmaxf(mx, __ldcg(at(p) + D));
-#pragma unroll (NG <= 2 ? 4 : 2)
-                for (int p = 0; p < parts; ++p) {
-                    const float2 ref = __ldcg(reinterpret_cast<const float2 *>(at(p) + D));
-                    const float f = ex2(ref.x - mx);
-                    lsum = fmaf(f, ref.y, lsum);
+                auto fetch = [&](int p0) {
 #pragma unroll
-                    for (int j = 0; j < NG; ++j) {
-                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(at(p) + j * 64 + 4 * c));
-                        sum[j].x = fmaf(f, v.x, sum[j].x); sum[j].y = fmaf(f, v.y, sum[j].y); sum[j].z = fmaf(f, v.z, sum[j].z); sum[j].w = fmaf(f, v.w, sum[j].w);
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int j = 0; j < NG; ++j) v[u][j] = __ldcg(reinterpret_cast<const float4 *>(at(min(p0 + u, parts - 1)) + j * 64 + 4 * c));
+                };
+                fetch(0);
+                float mx = fmaxf(ref0.x, ref1.x);
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(half, mx, d));
+                const float f0 = ex2(ref0.x - mx), f1 = ex2(ref1.x - mx);
+                float lsum = fmaf(f0, ref0.y, f1 * ref1.y);
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) lsum += __shfl_xor_sync(half, lsum, d);
+                for (int p0 = 0; p0 < parts; p0 += U) {
+                    if (p0 > 0) fetch(p0);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int p = p0 + u;
+                        const float f = __shfl_sync(half, p < 16 ? f0 : f1, p & 15, 16), to = p < parts ? f : 0.f;
+#pragma unroll
+                        for (int j = 0; j < NG; ++j) {
+                            sum[j].x = fmaf(to, v[u][j].x, sum[j].x); sum[j].y = fmaf(to, v[u][j].y, sum[j].y);
+                            sum[j].z = fmaf(to, v[u][j].z, sum[j].z); sum[j].w = fmaf(to, v[u][j].w, sum[j].w);
+                        }
                     }
                 }
                 if (final) {
@@ -889,7 +915,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
 #pragma unroll
                     for (int j = 0; j < NG; ++j) put(out, j, c, sum[j], inv);
                 } else {   // (a row's sixteen threads are of one warp: all have read before any writes)
-                    __syncwarp(0xffffu << (lane & 16));
+                    __syncwarp(half);
                     float *to = at(0);
 #pragma unroll
                     for (int j = 0; j < NG; ++j) *reinterpret_cast<float4 *>(to + j * 64 + 4 * c) = sum[j];
@@ -899,7 +925,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
             if (final) break;
             __syncthreads();
             first_part = piece0;
-            apart = kMeet;
+            apart = by;
             parts = groups;
             counter = a.counters + gridDim.x + piece0 / kMeet;   // (the first CTAs of two such jobs are more than kMeet apart)
         }
@@ -918,9 +944,9 @@ int launch(const AttnArgs &a, cudaStream_t stream)
     static PerDeviceOnce configured;
     if (cudaError_t e = configured.smem(S::kSmem, kern)) return fail(RMM_ERR_CUDA, "kv4_attn: cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     prof_begin("kv4_attn_kernel", stream);
-    // (counters: one a CTA, one for kMeet of them)
-    const int64_t ctas = (int64_t)sm_count() * S::kCtas, most = (kHeaderCounters - 4) * kMeet / (kMeet + 1) - 1;
-    launch_kernel(kern, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kWarps * 32), S::kSmem, stream, 1, a);
+    static_assert(kGrid + kGrid / kMeet + 1 <= kHeaderCounters, "a counter for each CTA and for kMeet of them");
+    const int64_t ctas = (int64_t)sm_count() * S::kCtas;
+    launch_kernel(kern, dim3((unsigned)(ctas < kGrid ? ctas : kGrid)), dim3(kWarps * 32), S::kSmem, stream, 1, a);
     return check_launch("kv4_attn_kernel", stream);
 }
 

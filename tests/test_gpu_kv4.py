@@ -223,6 +223,13 @@ def test_one_job_over_many_blocks_of_the_grid(pairs):
     check_attn([pairs * 32 - 5], 3, 1, 64, 64, 1, seed=pairs)
 
 
+@pytest.mark.parametrize("L", [1, 16])
+@pytest.mark.parametrize("pairs", [47, 96, 97, 224, 225, 240, 241, 247, 576, 577, 583, 1536, 1537, 1543, 2600, 2670, 3100])
+def test_one_job_in_pieces_that_meet_once_or_twice(pairs, L):
+    """Numbers of pieces around those where the way in which their sums meet changes; groups with one piece more than the others."""
+    check_attn([pairs * 32 - 7], 1, 1, 64, 128, L, seed=pairs)
+
+
 @pytest.mark.parametrize("q_scale, k_scale", [(30.0, 30.0), (1e-6, 1.0), (1e4, 1e-3), (1e-12, 1e12)])
 def test_logits_of_any_size(q_scale, k_scale):
     check_attn([200, 77], 4, 2, 128, 16, 2, q_scale=q_scale, k_scale=k_scale, seed=3)
