@@ -878,7 +878,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                 const float2 none = make_float2(-kNone, 0.f);
                 const float2 ref0 = c < parts ? __ldcg(reinterpret_cast<const float2 *>(at(c) + D)) : none;
                 const float2 ref1 = c + 16 < parts ? __ldcg(reinterpret_cast<const float2 *>(at(c + 16) + D)) : none;
-                constexpr int U = NG <= 2 ? 4 : 2;
+                constexpr int U = NG == 1 ? 8 : 16 / NG;
                 float4 sum[NG], v[U][NG];
 #pragma unroll
                 for (int j = 0; j < NG; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -886,7 +886,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
 #pragma unroll
                     for (int u = 0; u < U; ++u)
 #pragma unroll
-                        for (int j = 0; j < NG; ++j) v[u][j] = __ldcg(reinterpret_cast<const float4 *>(at(min(p0 + u, parts - 1)) + j * 64 + 4 * c));
+                        for (int j = 0; j < NG; ++j) {
+                            v[u][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (p0 + u < parts) v[u][j] = __ldcg(reinterpret_cast<const float4 *>(at(p0 + u) + j * 64 + 4 * c));
+                        }
                 };
                 fetch(0);
                 float mx = fmaxf(ref0.x, ref1.x);
@@ -933,8 +936,16 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     if (dead) drain_copies();
 }
 
-// Row tiles of 8, or of 16 where a kv head has more rows: they read the cache half as often.
-int row_tiles(const Kv4AttnProblem &p) { return p.Hq / p.Hkv * p.L <= 8 ? 1 : 2; }
+// Row tiles of 8, or of 16: those read the cache half as often, but the sums of a job that is cut take longer to meet.  What the
+// tiles of 8 would read is known by the table's room only.  (Tiles of 8 and 16, 32 + 8 heads of 128, 16 rows a kv head: one sequence
+// of 4096 14.0 and 17.4 us, four 18.4 and 18.5, eight 25.3 and 23.1; with 64 rows eight 96.4 and 51.4.  Heads of 256: 16 rows have no
+// room in the registers, 8 always took less: four sequences of 4096, 4 kv heads, 16 rows 18.4 and 32.8 us, 128 rows 63.4 and 81.1)
+constexpr int64_t kFewPairs = 64;   // an SM
+int row_tiles(const Kv4AttnProblem &p, const kv4::View &cache)
+{
+    const int64_t rows = p.Hq / p.Hkv * p.L, pairs = (cache.max_pages << cache.page_shift) / 2 + 1;
+    return rows <= 8 || p.D == 256 || (double)p.B * p.Hkv * ceil_div(rows, 8) * pairs <= (double)(sm_count() * kFewPairs) ? 1 : 2;
+}
 
 template <int D, int NT>
 int launch(const AttnArgs &a, cudaStream_t stream)
@@ -955,12 +966,12 @@ int launch(const AttnArgs &a, cudaStream_t stream)
 bool kv4_attn_fits(const Kv4AttnProblem &p, const kv4::View &cache)
 {
     // the axis of all pairs, and with it a number below that of the grid's blocks, is counted in 32 bits
-    const double chunks = (double)ceil_div(p.Hq / p.Hkv * p.L, 8 * row_tiles(p));
+    const double chunks = (double)ceil_div(p.Hq / p.Hkv * p.L, 8 * row_tiles(p, cache));
     return (double)p.B * p.Hkv * chunks * (0.5 * (double)(cache.max_pages << cache.page_shift) + 1.0 + kFixed) < 2147000000.0 && p.Hq / p.Hkv * p.L < INT32_MAX / 2 &&
            p.B * p.Hq < INT32_MAX;
 }
 
-static size_t parts_bytes(const Kv4AttnProblem &p) { return align_up((size_t)sm_count() * 4 * 8 * row_tiles(p) * (p.D + 4) * 4, 256); }
+static size_t parts_bytes(const Kv4AttnProblem &p) { return align_up((size_t)kGrid * (p.D == 256 ? 8 : 16) * (p.D + 4) * 4, 256); }
 
 size_t kv4_attn_workspace_bytes(const Kv4AttnProblem &p)
 {
@@ -970,7 +981,7 @@ size_t kv4_attn_workspace_bytes(const Kv4AttnProblem &p)
 int launch_kv4_attn(const Kv4AttnProblem &p, const kv4::View &cache, float *scratch, unsigned *counters, int *status, cudaStream_t stream)
 {
     AttnArgs a = {};
-    const int nt = row_tiles(p);
+    const int nt = row_tiles(p, cache);
     a.q = static_cast<const __nv_bfloat16 *>(p.q);
     a.o = static_cast<__nv_bfloat16 *>(p.o);
     a.q_sb = p.q_sb; a.q_sh = p.q_sh; a.q_sr = p.q_sr;
@@ -999,7 +1010,7 @@ int launch_kv4_attn(const Kv4AttnProblem &p, const kv4::View &cache, float *scra
     }
     if (p.D == 64) return nt == 1 ? launch<64, 1>(a, stream) : launch<64, 2>(a, stream);
     if (p.D == 128) return nt == 1 ? launch<128, 1>(a, stream) : launch<128, 2>(a, stream);
-    return nt == 1 ? launch<256, 1>(a, stream) : launch<256, 2>(a, stream);
+    return launch<256, 1>(a, stream);
 }
 
 }  // namespace rmm

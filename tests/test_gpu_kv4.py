@@ -207,6 +207,35 @@ def test_attention_matches_64_bits(lengths, Hq, Hkv, page, L, new, causal, rho_d
     check_attn(lengths, Hq, Hkv, D, page, L, new, causal, rho_d, seed=D + L)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("lengths, Hq, Hkv, page, L, new, causal, rho_d", [
+    ([15, 16, 17, 0, 33], 12, 1, 16, 1, None, True, 1.0),
+    ([1], 9, 1, 16, 1, None, True, 1.0),
+    ([300, 5, 90], 6, 2, 16, 5, None, True, 0.3),
+    ([300, 5, 90, 7], 4, 1, 16, 7, [7, 2, 0, 7], True, 0.7),
+    ([257, 31], 16, 1, 128, 3, None, False, 1.0),
+    ([120, 400], 2, 2, 16, 16, None, True, 0.5),
+    ([150, 40], 4, 2, 16, 40, [40, 33], True, 1.0),
+    ([4099, 40], 10, 1, 64, 1, None, True, 0.5),
+    ([9000], 16, 1, 64, 1, None, True, 1.0),
+])
+def test_tables_with_room_for_many_more_tokens(lengths, Hq, Hkv, page, L, new, causal, rho_d, D):
+    """The room of a table decides how many rows read the keys at a time; its entries behind a sequence's end are not looked at."""
+    pool, table, K, V = filled(lengths, Hkv, D, page, seed=D + L)
+    wide = torch.full((len(lengths), (1 << 20) // page), -1, dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    Q = torch.randn(len(lengths), Hq, L, D, generator=gen(7)).to(BF16)
+    if new is not None:   # rows that are none may hold anything
+        for b, n in enumerate(new):
+            Q[b, :, n:] = torch.tensor([float("nan"), float("inf")]).repeat(D // 2).to(BF16)
+    got = rmm.rmm_kv4_attn(Q.cuda(), pool, wide.cuda(), ints(lengths), None if new is None else ints(new), causal=causal, rho_d=rho_d)
+    narrow = rmm.rmm_kv4_attn(Q.cuda(), pool, table.cuda(), ints(lengths), None if new is None else ints(new), causal=causal, rho_d=rho_d)
+    assert rmm.rmm_status_read() == 0
+    Q = torch.nan_to_num(Q.float(), 0.0, 0.0, 0.0).to(BF16)
+    for O in (got, narrow):
+        compare(O, None, Q, K, V, lengths, [L] * len(lengths) if new is None else new, causal, rho_d)
+
+
 def test_many_short_and_some_long_sequences():
     """More sequences than a CTA has threads, most of them a few tokens long; jobs that lie inside a CTA and jobs that many share."""
     lengths = [(7 * i) % 40 for i in range(600)]
