@@ -149,17 +149,17 @@ __device__ __forceinline__ void job_next(const AttnArgs &a, Job &c, int limit)  
     }
 }
 
-// Kept features of one head a warp, as bit masks; the rule of every other form: squares summed in fp64, rounded to fp32, the kd
-// largest, the lower index first.
+// Kept features of one head a block, as bit masks; the rule of every other form: squares summed in fp64, rounded to fp32, the kd
+// largest, the lower index first.  (Blocks of one warp: four of them have no room beside the attention's, which then start late.  24 sequences
+// of up to 16384, 16 + 4 heads of 256, half of the features: 30.6 us, with blocks of two or four warps 34.9; all features 24.3)
 template <int W32>
-__global__ void __launch_bounds__(128) kv4_features_kernel(const __grid_constant__ AttnArgs a, uint32_t *kept, int32_t *idx_feat)
+__global__ void __launch_bounds__(32) kv4_features_kernel(const __grid_constant__ AttnArgs a, uint32_t *kept, int32_t *idx_feat)
 {
     // The attention may start once everything before this kernel is complete: it waits for the masks only where it reads them
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t job = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), Hq = (int64_t)a.Hkv * a.group;
-    if (job >= a.B * Hq) return;
+    const int lane = threadIdx.x;
+    const int64_t job = blockIdx.x, Hq = (int64_t)a.Hkv * a.group;
     const int64_t b = job / Hq, h = job - b * Hq;
     int len, rows;
     kv4::sequence(a.cache, b, len, rows, a.status);
@@ -386,22 +386,22 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     Raw8<__nv_bfloat16> q_raw[QT];
     uint32_t q_kept[QT];
     auto q_row = [&](int k) { return (k * THREADS + tid) / QL; };
-    auto load_q = [&]() {
+    auto load_q = [&](bool raw, bool kept) {
         const Job cur = s_cur;
         const int row0 = cur.chunk * ROWS, nrows = min(ROWS, cur.rows * a.group - row0), c = tid % QL;
 #pragma unroll
         for (int k = 0; k < QT; ++k) {
             const int r = q_row(k), i = (row0 + r) / a.group;
-            q_raw[k] = zero_raw<__nv_bfloat16>();
-            q_kept[k] = 0xffu;
-            if (r < nrows) {
-                const int64_t head = (int64_t)cur.hk * a.group + row0 + r - i * a.group;
-                q_raw[k] = load_raw(a.q + cur.b * a.q_sb + head * a.q_sh + (int64_t)i * a.q_sr + 8 * c, a.q_vec != 0);
-                if (a.kept != nullptr) q_kept[k] = a.kept[((int64_t)cur.b * a.Hkv * a.group + head) * W32 + c / 4] >> (8 * (c % 4));
+            const int64_t head = (int64_t)cur.hk * a.group + row0 + r - i * a.group;
+            if (raw) {
+                q_raw[k] = zero_raw<__nv_bfloat16>();
+                if (r < nrows) q_raw[k] = load_raw(a.q + cur.b * a.q_sb + head * a.q_sh + (int64_t)i * a.q_sr + 8 * c, a.q_vec != 0);
             }
+            q_kept[k] = 0xffu;
+            if (kept && r < nrows) q_kept[k] = __ldcg(a.kept + ((int64_t)cur.b * a.Hkv * a.group + head) * W32 + c / 4) >> (8 * (c % 4));
         }
     };
-    if (a.kept == nullptr) load_q();
+    load_q(true, false);
 
     // ---- the warp's loads: pairs first + warp, + 4, .. of every part, ST of them under way
     int p_start = start, p_t = 0, p_end = 0, p_k = 64, p_slot = 0;
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     for (int i = 0; i < ST; ++i) request();
     if (a.kept != nullptr) {
         pdl_wait();
-        load_q();
+        load_q(false, true);
     }
 
     // columns 64 j + 8 (2 (c % 4)) + 2 (c / 4), the next, and those 8 on, of an output row
@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         const int t0 = first_pair, t1 = min(s_cur.nb, end_pair), cost = s_cur.cost();
         {
             // ---- Q scaled to fp16
-            if (!first) load_q();
+            if (!first) load_q(true, a.kept != nullptr);
             int vis_least;
             {
             const Job cur = s_cur;
@@ -1004,7 +1004,7 @@ int launch_kv4_attn(const Kv4AttnProblem &p, const kv4::View &cache, float *scra
         uint32_t *kept = reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(scratch) + parts_bytes(p));
         auto kern = p.D == 64 ? kv4_features_kernel<2> : (p.D == 128 ? kv4_features_kernel<4> : kv4_features_kernel<8>);
         prof_begin("kv4_features_kernel", stream);
-        launch_kernel(kern, dim3((unsigned)ceil_div(p.B * p.Hq, 4)), dim3(128), 0, stream, 1, a, kept, p.idx_feat);
+        launch_kernel(kern, dim3((unsigned)(p.B * p.Hq)), dim3(32), 0, stream, 1, a, kept, p.idx_feat);
         if (int rc = check_launch("kv4_features_kernel", stream)) return rc;
         a.kept = kept;
     }
