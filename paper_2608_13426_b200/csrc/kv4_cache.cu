@@ -86,9 +86,10 @@ __device__ __forceinline__ uint32_t pack_pair(float s, float m) { return __byte_
 __device__ __forceinline__ void dequantise8(uint32_t codes, uint32_t pair, Eight &x)
 {
     const uint64_t s = both(bf16_bits(pair)), m = both(__uint_as_float(pair & 0xffff0000u));
+    const uint32_t even = codes & 0x0f0f0f0fu, odd = codes >> 4 & 0x0f0f0f0fu;   // a byte each: 2^23 + n is three bytes and that
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint64_t n = ptx::pack2(__uint_as_float((codes >> (8 * i) & 15u) | 0x4b000000u), __uint_as_float((codes >> (8 * i + 4) & 15u) | 0x4b000000u));
+        const uint64_t n = ptx::pack2(__uint_as_float(__byte_perm(even, 0x4b000000u, 0x7550 + i)), __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7550 + i)));
         x[i] = ptx::ffma2(s, ptx::fadd2(n, both(-8388608.f)), m);
     }
 }
