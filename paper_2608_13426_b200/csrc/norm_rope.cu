@@ -4,6 +4,8 @@
 // Bound: HBM, each head read and written once.  A row's columns sit in neighbouring lanes, eight each (16 bytes of bf16), so a
 // row never leaves its lanes: squares meet by shuffles, pairs are exchanged by shuffles.  A warp takes one token and several heads: its
 // cosines, sines and weights are read once and stay in registers (a table's row is as large as two heads).
+// Measured: 2 x 4096 tokens of 32 + 8 heads of 128, bf16: 36.5 us for 172 MB (4.7 TB/s; 26.6 us at the copy rate).  136 warp
+// instructions for two rows fill half of the issue slots, logical operations 44 % of their pipe, and loads wait behind them.
 #include <type_traits>
 
 #include "heads.cuh"
