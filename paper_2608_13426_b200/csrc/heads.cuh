@@ -292,8 +292,8 @@ static __device__ __noinline__ uint32_t element_64(float x, float xp, double r, 
 // r (10 u |x a| + 11 u |x' b|): a sum of up to 256 squares in chains of four, one sum of two and up to five meetings, mean and eps (11
 // roundings, of which the root halves the effect), rsqrtf after one step of Newton's (1), a and b (1), two products (2), the scaling (1);
 // e is 12 u.  A column where z - e and z + e round to different numbers, one of 1500 or so, is done again in 64 bits; so is a row whose
-// squares leave the range of fp32.  (4 x 4096 tokens, 8 heads of 128 appended in 44 us, where whole rows were
-// done again in 62.)
+// squares leave the range of fp32.  (Appending 4 x 4096 rows of 8 heads of 128 took 62 us where such
+// a column's whole row was done again, 44 since.)
 template <int LANES, typename T>
 __device__ __forceinline__ void norm_rope_row_bf16(const Raw8<T> &raw, const RowLane &k, const void *weight, const RopeView &rope, int64_t position,
                                                    int col, uint32_t (&out)[4])
