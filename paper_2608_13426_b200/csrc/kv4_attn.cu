@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     constexpr int ROWS = S::kRows, NG = S::kGroups, ST = S::kStages, W32 = D / 32, THREADS = kWarps * 32;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ Job s_cur, s_pc[kWarps];   // the job at hand, and the one that a warp asks for (kept out of the registers of the loop over the keys)
-    __shared__ float s_need[kLimits][kWarps];
+    __shared__ int s_need[kLimits][kWarps];
     __shared__ int s_scan[2][kWarps], s_begin[2], abort_flag, s_last;
     int64_t *row_out = reinterpret_cast<int64_t *>(smem + S::kOffOut);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
@@ -263,9 +263,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
     const int share = max(kLeast, (total + (int)gridDim.x - 1) / (int)gridDim.x);
     int limit = share;
     {
-        // CTAs that a limit asks for, a limit a lane of eight
+        // CTAs that a limit asks for, in 2^-16, a limit a lane of eight: some more than whole pieces where jobs are left that are not cut
         const int t = share * kLimit[tid % kLimits] / 16;
-        float need = 0.f;
+        int need = 0;
         for (int b0 = 0; b0 < a.B; b0 += THREADS) {
             if (a.B > THREADS) {
                 __syncthreads();
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
                 const int4 q = s_seq[i];
                 const bool cut = q.x > t;
                 const float rest = (float)(cut ? a.chunks - q.z : q.w);
-                need += (cut ? (float)q.z * (float)pieces_of(q.y, t) : 0.f) + __fdividef(rest, (float)t);
+                need += (cut ? q.z * pieces_of(q.y, t) << 16 : 0) + (rest > 0.f ? (int)__fdividef(65536.f * rest, (float)t) + 1 : 0);
             }
         }
 #pragma unroll
@@ -285,10 +285,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT>::kCtas) kv4_attn_ker
         __syncthreads();
 #pragma unroll
         for (int k = kLimits - 1; k >= 0; --k) {
-            float v = 0.f;
+            int v = 0;   // (below 2^31: no limit asks for more than five times the CTAs, and a job adds one at most)
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) v += s_need[k][w];
-            if (k == kLimits - 1 || v * (float)a.Hkv <= (float)gridDim.x - 0.01f) limit = share * kLimit[k] / 16;
+            if (k == kLimits - 1 || v * a.Hkv <= (int)gridDim.x << 16) limit = share * kLimit[k] / 16;
         }
     }
     // CTAs with a piece of a job, and what the other jobs count: this thread's sequence, the sequences up to it, all

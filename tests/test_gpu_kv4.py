@@ -252,6 +252,13 @@ def test_one_job_over_many_blocks_of_the_grid(pairs):
     check_attn([pairs * 32 - 5], 3, 1, 64, 64, 1, seed=pairs)
 
 
+@pytest.mark.parametrize("sequences", [36, 37, 38])
+def test_pieces_that_fill_the_grid(sequences):
+    """148 jobs of three pieces are as many as the blocks that 148 SMs hold, and no block is left for jobs that are not cut."""
+    check_attn([1500] * sequences, 4, 4, 64, 64, 1, seed=3)
+    check_attn([1500] * sequences + [3], 4, 4, 64, 64, 1, seed=4)
+
+
 @pytest.mark.parametrize("L", [1, 16])
 @pytest.mark.parametrize("pairs", [47, 96, 97, 224, 225, 240, 241, 247, 576, 577, 583, 1536, 1537, 1543, 2600, 2670, 3100])
 def test_one_job_in_pieces_that_meet_once_or_twice(pairs, L):
